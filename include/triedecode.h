@@ -16,6 +16,12 @@
  * beam_topk_append does the last two in one call (same results).  trie_tree_attn runs
  * the same attention with any set of stored nodes as queries (a prefill, or draft nodes).
  *
+ * Requests that begin alike (a system prompt, examples, a document) can share that beginning:
+ * td_set_prefix attaches a prefix in a paged cache to every trie of the context, trie_prefix_store
+ * and trie_prefix_attn are its own prefill, and the attention of the tries then runs over the
+ * prefix, once for all of them, and over their own nodes.  trie_store_kv rotates queries and keys
+ * to the nodes' positions and stores their rows.
+ *
  * Memory.  The caller owns every tensor (K/V pools, queries, outputs, logits and
  * selections) as device memory; PyTorch tensors are the intended source.  The library
  * owns only the trie metadata and a fixed workspace, both allocated in td_create.  The
@@ -151,7 +157,7 @@ td_status td_init_prompt(td_ctx* ctx, const int32_t* h_prompt_len, const int32_t
  * reads KV head h / (Hq/Hkv).  When the leaves' K/V are pending (after an append), the
  * call first copies the rows the append's compaction moved (layers not done yet), then
  * stores k_new/v_new into the leaves' pool rows, and the leaves attend to them;
- * otherwise d_k_new/d_v_new must be NULL.  fp32 accumulation; out rows of beams
+ * otherwise (or after trie_store_kv of every layer of the call) d_k_new/d_v_new must be NULL.  fp32 accumulation; out rows of beams
  * >= n_live are zeroed.  scale is normally 1/sqrt(d). */
 td_status trie_attn_decode(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, const void* d_q,
                            const void* d_k_new, const void* d_v_new, void* d_out, float scale,
@@ -175,6 +181,72 @@ td_status trie_attn_decode(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, c
 td_status trie_tree_attn(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t q_max,
                          const int32_t* d_qslots, const void* d_q, void* d_out, float scale,
                          hipStream_t stream);
+
+/* A paged cache that holds a prefix: positions i * page_size .. of it are the rows of page
+ * h_page_table[i].  The caller owns the pages; a pool may hold those of several prefixes. */
+typedef struct {
+  void* k_pages;               /* device [n_pages][L][Hkv][page_size][d], desc.dtype, 16-byte       */
+  void* v_pages;               /*   aligned; valid until the prefix is replaced or td_destroy        */
+  int32_t n_pages;             /* pages of the pool                                                 */
+  int32_t page_size;           /* positions per page: a power of two in [16, 65536]                 */
+  const int32_t* h_page_table; /* host [n_table]: distinct pages in [0, n_pages)                    */
+  int32_t n_table;             /* n_table * page_size positions can be stored (at most 2^30)         */
+  int32_t length;              /* S in [0, n_table * page_size]: the positions the tries attend to   */
+} td_prefix;
+
+/* Attach a prefix to every trie of the context (NULL: detach), from the next call on.  Position j
+ * < S precedes every node: a node of depth D is at position S + D, in the rotation of trie_store_kv
+ * and in the window.  The tries' stored rows are left as they are: attach before rows that depend
+ * on the positions are stored, and re-attach a longer table or length when the prefix grows.
+ * trie_attn_decode and trie_tree_attn then attend to the prefix's positions too: position p is
+ * visible to a query at depth D iff S + D - p < W when a window is set.  Host arrays are copied.
+ * Synchronises the device and may allocate (the table, and with the first prefix a workspace of two
+ * times 64 MiB, or what one layer of a decode step needs); not for use under capture.  A captured
+ * attention call of a context with a prefix (length >= 1) reads the one attached when it is
+ * replayed; one captured without stays without. */
+td_status td_set_prefix(td_ctx* ctx, const td_prefix* prefix);
+
+/* A rotary position embedding: pair i of a head's first `dim` elements turns by position *
+ * d_freq[i]: (x, y) -> (x cos - y sin, y cos + x sin); the elements past dim are copied. */
+typedef struct {
+  const float* d_freq;  /* device [dim / 2], radians per position                                  */
+  int32_t dim;          /* a multiple of 16 in [16, d]                                             */
+  int32_t interleaved;  /* 0: pair i is elements (i, i + dim / 2); 1: (2i, 2i + 1)                  */
+} td_rope;
+
+/* Store n tokens of the prefix at positions pos .. pos + n - 1 (inside the table; `length` plays no
+ * part), for layers [layer_begin, +n_layers): K rotated to its position (rope NULL: as it is) and V
+ * go to their pages, q rotated to q_out.  Either of (q, q_out) and (k, v) may be NULL; q_out may be
+ * q.  Rows [nl][n][heads][d], where consecutive rows lie q_stride (k_stride, v_stride) elements
+ * apart - a slice of a fused projection's output does - at least heads * d and a multiple of 8;
+ * 0: contiguous.  q_out [nl][n][Hq][d] is contiguous.  Angles are computed in 64 bits; results are
+ * rounded once, to desc.dtype.  Needs an attached prefix (else TD_ESTATE), but no prompts. */
+td_status trie_prefix_store(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n,
+                            const td_rope* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
+                            const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t stream);
+
+/* Causal attention of n tokens of the prefix (its prefill, whole or in chunks): the query of token
+ * j, at position pos + j, attends to the stored positions p <= pos + j with pos + j - p < W when a
+ * window is set.  d_q, d_out [nl][n][Hq][d]; pos + n inside the table, every position up to there
+ * stored, n * (Hq/Hkv) <= 2^24.  Needs an attached prefix (else TD_ESTATE), but no prompts.  Every
+ * type and head dim. */
+td_status trie_prefix_attn(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n, const void* d_q,
+                           void* d_out, float scale, hipStream_t stream);
+
+/* Store rows of the tries' nodes, for layers [layer_begin, +n_layers): K rotated to the node's
+ * position, S + its depth (S = 0 without a prefix; rope NULL: as it is), and V go to the node's pool
+ * row, q rotated to q_out.  Arguments as in trie_prefix_store, rows [nl][T][q_max][heads][d].
+ *   d_qslots [T][q_max] (device): the nodes by logical slot, as in trie_tree_attn (a prefill, or
+ *   draft nodes).  A row with no node (-1, or a slot past the last) stores nothing, and its q_out is
+ *   zero.  The slots of one trie must be distinct when K/V are given (else which row's chunks a node
+ *   gets is unspecified).  TD_ESTATE while the leaves' rows are pending.
+ *   d_qslots NULL: the live leaves in rank order, q_max = b; rows of beams >= n_live store nothing,
+ *   and their q_out is zero.  With K/V this is the store that trie_attn_decode does from k_new /
+ *   v_new (rows moved by a collection are copied first): the layers' rows are no longer pending, and
+ *   trie_attn_decode of these layers takes NULL k_new / v_new. */
+td_status trie_store_kv(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t q_max, const int32_t* d_qslots,
+                        const td_rope* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
+                        const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t stream);
 
 /* Phases of a decode step that td_set_kernel_events can time. */
 typedef enum {

@@ -44,6 +44,16 @@ class BbsDesc(ctypes.Structure):
                 ("k_cache", ctypes.c_void_p * 2), ("v_cache", ctypes.c_void_p * 2)]
 
 
+class TdPrefix(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("h_page_table", ctypes.POINTER(ctypes.c_int32)),
+                ("n_table", ctypes.c_int32), ("length", ctypes.c_int32)]
+
+
+class TdRope(ctypes.Structure):
+    _fields_ = [("d_freq", ctypes.c_void_p), ("dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
 class TdState(ctypes.Structure):
     _fields_ = [("n_nodes", ctypes.c_int32), ("n_live", ctypes.c_int32), ("base", ctypes.c_int32),
                 ("n_shared", ctypes.c_int32), ("next_id", ctypes.c_int32),
@@ -87,6 +97,11 @@ def lib() -> ctypes.CDLL:
         L.td_set_kernel_events.argtypes = [vp, i32, vp, vp]
         L.td_read_finished.argtypes = [vp, i32, vp, vp, vp, vp, ctypes.POINTER(i32), ctypes.POINTER(i32)]
         L.trie_tree_attn.argtypes = [vp, i32, i32, i32, vp, vp, vp, f32, vp]
+        L.td_set_prefix.argtypes = [vp, ctypes.POINTER(TdPrefix)]
+        i64, rope = ctypes.c_int64, ctypes.POINTER(TdRope)
+        L.trie_prefix_store.argtypes = [vp, i32, i32, i32, i32, rope, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.trie_store_kv.argtypes = [vp, i32, i32, i32, vp, rope, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.trie_prefix_attn.argtypes = [vp, i32, i32, i32, i32, vp, vp, f32, vp]
         L.td_error_string.argtypes = [vp]
         L.td_error_string.restype = ctypes.c_char_p
         L.beam_topk_static.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
@@ -107,7 +122,8 @@ def lib() -> ctypes.CDLL:
         for name in ("td_create", "td_destroy", "td_init_prompt", "trie_attn_decode",
                      "beam_logsoftmax_topk", "beam_topk_append", "beam_topk_static", "td_read_probe", "trie_append_prune",
                      "td_read_state", "td_load_state",
-                     "td_get_status", "td_set_kernel_events", "td_read_finished", "trie_tree_attn", "bbs_create", "bbs_destroy",
+                     "td_get_status", "td_set_kernel_events", "td_read_finished", "trie_tree_attn",
+                     "td_set_prefix", "trie_prefix_store", "trie_store_kv", "trie_prefix_attn", "bbs_create", "bbs_destroy",
                      "bbs_init_prompt", "batch_beam_attn_decode", "batch_beam_logsoftmax_topk",
                      "batch_beam_reorder", "bbs_current_cache", "bbs_read_beams", "bbs_get_status"):
             getattr(L, name).restype = ctypes.c_int32
@@ -202,6 +218,101 @@ def trie_tree_attn(ctx, dims: Dims, layer_begin: int, n_layers: int, qslots, q, 
     _check(ctx, lib().trie_tree_attn(ctx, int(layer_begin), int(n_layers), qmax,
                                      _ptr(qslots, torch.int32, dims.T * qmax, "qslots"), _ptr(q, tdt, nq, "q"),
                                      _ptr(out, tdt, nq, "out"), float(scale), _stream(stream)))
+
+
+class Rope:
+    """A rotary embedding (td_rope): freq, float32 device tensor of the pairs' radians per position;
+    interleaved pairs are (2i, 2i + 1), else (i, i + len(freq))."""
+
+    def __init__(self, freq, interleaved: bool = False):
+        import torch
+        _ptr(freq, torch.float32, name="freq")
+        self.freq = freq  # (keeps the tensor alive)
+        self.c = TdRope(freq.data_ptr(), 2 * freq.numel(), int(bool(interleaved)))
+
+
+def td_set_prefix(ctx, dims: Dims, k_pages, v_pages=None, pages: Sequence[int] = (), length: int = 0):
+    """Attach a prefix (k_pages None: detach): k_pages / v_pages [n_pages][L][Hkv][page_size][d] device
+    tensors, pages the table (position i lies in page pages[i // page_size])."""
+    if k_pages is None:
+        _check(ctx, lib().td_set_prefix(ctx, None))
+        return
+    import torch
+    tdt = torch.float32 if dims.dtype == TD_F32 else torch.bfloat16
+    if k_pages.dim() != 5 or tuple(k_pages.shape[1:3]) != (dims.L, dims.Hkv) or k_pages.shape[4] != dims.D:
+        raise ValueError("k_pages must be [n_pages][n_layers][n_kv_heads][page_size][head_dim]")
+    table = np.ascontiguousarray(np.asarray(pages, dtype=np.int32))
+    if table.ndim != 1 or not np.array_equal(table, np.asarray(pages)):
+        raise ValueError("pages must be a sequence of 32-bit integers")
+    d = TdPrefix(_ptr(k_pages, tdt, None, "k_pages"), _ptr(v_pages, tdt, k_pages.numel(), "v_pages"),
+                 int(k_pages.shape[0]), int(k_pages.shape[3]), table.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)),
+                 table.size, int(length))
+    _check(ctx, lib().td_set_prefix(ctx, ctypes.byref(d)))
+
+
+def _rows(t, dtype, lead, heads, dim, name):
+    """Address and row stride of t [lead..][heads][dim]: a device tensor whose rows are contiguous and
+    follow one another at one distance (a slice of a fused projection)."""
+    if t is None:
+        return None, 0
+    shape = tuple(lead) + (heads, dim)
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be a device tensor of {dtype} and shape {list(shape)}, got {t.dtype}, {list(t.shape)}")
+    rows = [(n, st) for n, st in zip(t.shape[:-2], t.stride()[:-2]) if n != 1]
+    row = rows[-1][1] if rows else heads * dim
+    ok = (dim == 1 or t.stride(-1) == 1) and (heads == 1 or t.stride(-2) == dim)
+    for n, st in reversed(rows):
+        ok = ok and st == row
+        row *= n
+    if not ok:
+        raise ValueError(f"{name}: rows must be contiguous and equally far apart, got strides {t.stride()}")
+    return t.data_ptr(), rows[-1][1] if rows else heads * dim
+
+
+def _store_rows(dims: Dims, lead, k, v, q, q_out):
+    import torch
+    tdt = torch.float32 if dims.dtype == TD_F32 else torch.bfloat16
+    (qp, qs), (kp, ks), (vp, vs) = (_rows(q, tdt, lead, dims.Hq, dims.D, "q"), _rows(k, tdt, lead, dims.Hkv, dims.D, "k"),
+                                    _rows(v, tdt, lead, dims.Hkv, dims.D, "v"))
+    n = dims.Hq * dims.D
+    for x in lead:
+        n *= x
+    return qp, qs, kp, ks, vp, vs, _ptr(q_out, tdt, n, "q_out")
+
+
+def trie_prefix_store(ctx, dims: Dims, layer_begin: int, n_layers: int, pos: int, k, v, q=None, q_out=None,
+                      rope: Optional[Rope] = None, stream=None):
+    """Store tokens pos, pos + 1, ... of the prefix: k / v [n_layers][n][Hkv][d] (k rotated), q
+    [n_layers][n][Hq][d] rotated to q_out; their rows may be slices of a wider tensor's."""
+    n = int((q if k is None else k).shape[1])
+    args = _store_rows(dims, (n_layers, n), k, v, q, q_out)
+    _check(ctx, lib().trie_prefix_store(ctx, int(layer_begin), int(n_layers), int(pos), n,
+                                        None if rope is None else ctypes.byref(rope.c), *args, _stream(stream)))
+
+
+def trie_store_kv(ctx, dims: Dims, layer_begin: int, n_layers: int, k, v, q=None, q_out=None,
+                  rope: Optional[Rope] = None, qslots=None, stream=None):
+    """Store rows of the live leaves (k / v [n_layers][T][b][Hkv][d]) or of the nodes qslots [T][q_max]
+    (k / v [n_layers][T][q_max][Hkv][d]), rotated to the nodes' positions; q to q_out likewise."""
+    import torch
+    if qslots is not None and (qslots.dim() != 2 or qslots.shape[0] != dims.T):
+        raise ValueError("qslots must be [T][q_max]")
+    n = dims.b if qslots is None else int(qslots.shape[1])
+    args = _store_rows(dims, (n_layers, dims.T, n), k, v, q, q_out)
+    _check(ctx, lib().trie_store_kv(ctx, int(layer_begin), int(n_layers), n, _ptr(qslots, torch.int32, None, "qslots"),
+                                    None if rope is None else ctypes.byref(rope.c), *args, _stream(stream)))
+
+
+def trie_prefix_attn(ctx, dims: Dims, layer_begin: int, n_layers: int, pos: int, q, out, scale: float, stream=None):
+    """Causal attention of the prefix's tokens pos, pos + 1, ...: q / out [n_layers][n][Hq][d]."""
+    import torch
+    tdt = torch.float32 if dims.dtype == TD_F32 else torch.bfloat16
+    if q.dim() != 4:
+        raise ValueError("q must be [n_layers][n][n_q_heads][head_dim]")
+    n = int(q.shape[1])
+    nq = n_layers * n * dims.Hq * dims.D
+    _check(ctx, lib().trie_prefix_attn(ctx, int(layer_begin), int(n_layers), int(pos), n, _ptr(q, tdt, nq, "q"),
+                                       _ptr(out, tdt, nq, "out"), float(scale), _stream(stream)))
 
 
 def td_set_kernel_events(ctx, phase, start, stop):
@@ -425,6 +536,19 @@ class TrieDecoder:
 
     def tree_attn(self, layer_begin, n_layers, qslots, q, out, scale, stream=None):
         trie_tree_attn(self.ctx, self.dims, layer_begin, n_layers, qslots, q, out, scale, stream)
+
+    def set_prefix(self, k_pages, v_pages=None, pages=(), length=0):
+        td_set_prefix(self.ctx, self.dims, k_pages, v_pages, pages, length)
+        self.prefix_pages = (k_pages, v_pages)  # (kept alive while attached)
+
+    def prefix_store(self, layer_begin, n_layers, pos, k, v, q=None, q_out=None, rope=None, stream=None):
+        trie_prefix_store(self.ctx, self.dims, layer_begin, n_layers, pos, k, v, q, q_out, rope, stream)
+
+    def prefix_attn(self, layer_begin, n_layers, pos, q, out, scale, stream=None):
+        trie_prefix_attn(self.ctx, self.dims, layer_begin, n_layers, pos, q, out, scale, stream)
+
+    def store_kv(self, layer_begin, n_layers, k, v, q=None, q_out=None, rope=None, qslots=None, stream=None):
+        trie_store_kv(self.ctx, self.dims, layer_begin, n_layers, k, v, q, q_out, rope, qslots, stream)
 
     def status(self):
         return td_get_status(self.ctx)

@@ -678,7 +678,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_mfma(DevState s, AttnArgs a
         O[4] += x1.x * f; O[5] += x1.y * f; O[6] += x1.z * f; O[7] += x1.w * f;
       }
       const float Mi = rowm[i], L = rowl[i];
-      if (a.splits == 1) {
+      if (!a.partial) {
         const int rr = (u.rb * RB + rbk) * kRows + i;
         if (rr < nrows * G) {
           const int bm = rr / G;

@@ -413,7 +413,7 @@ __global__ __launch_bounds__((Cfg32<T, D, RT>::NW * 64), (Cfg32<T, D, RT>::NW / 
       O += *reinterpret_cast<const f32x4*>(obuf + (w * C::ROWS + i) * C::OS + c) * f;
     }
     const float L = rowl[i];
-    if (a.splits == 1) {
+    if (!a.partial) {
       const int r = u.rb * C::ROWS + i;
       if (r < s.b * G) {
         const int bm = r / G;

@@ -63,7 +63,7 @@ struct TreeCfg : TreeGeom<D> {
 
 // KS: groups of 4 waves that share the rows and split the keys, tile by tile (group k takes
 // tiles k, k + KS, ...); their states are merged at the end.
-template <int D, int KS>
+template <int D, int KS, bool PFX>
 __global__ __launch_bounds__(KS * kTreeThreads, TreeCfg<D>::WAVES) void k_attn_tree(DevState s, AttnArgs a) {
   using C = TreeCfg<D>;
   // K and V of two tiles.  Four arrays, each used for one buffer only: the compiler can then
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(KS * kTreeThreads, TreeCfg<D>::WAVES) void k_attn_t
   const uint64_t* maskp = s.mask + (size_t)u.t * s.cap + base;
   const int32_t* depthp = s.depth + (size_t)u.t * s.cap + base;
 
-  const TreeRow q = tree_row(s, a, u, N, G, maskp, depthp, wave, col);
+  const TreeRow q = tree_row<PFX>(s, a, u, N, G, maskp, depthp, wave, col);
   const int2 range = tree_range(s, u, q, base, N, lane, wave, wred);
   const int lo = range.x, hi = range.y;
   const int ntiles = hi > lo ? (hi - lo + 63) / 64 : 0;
@@ -294,6 +294,7 @@ __global__ __launch_bounds__(KS * kTreeThreads, TreeCfg<D>::WAVES) void k_attn_t
     const float m1 = ml[(wave * 2) * 64 + lane], l1 = ml[(wave * 2 + 1) * 64 + lane];
     const float mn = fmaxf(m, m1);
     const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(m1 - mn);
+    m = mn;
     lsum = lsum * f0 + l1 * f1;
 #pragma unroll
     for (int x = 0; x < D / 4; ++x) {
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(KS * kTreeThreads, TreeCfg<D>::WAVES) void k_attn_t
     }
   }
 
-  tree_output<D>(s, a, u, q, G, hh, lsum, o);
+  tree_output<D, PFX>(s, a, u, q, G, hh, m, lsum, o);
 }
 
 }  // namespace
@@ -335,9 +336,10 @@ hipError_t launch_attn_tree(const DevState& s, const AttnArgs& a, long max_keys,
   if (max_keys <= kTreeShortKeys || (s.D == 64 && max_keys <= kTreeShortKeys64 && !split))
     return launch_attn_tree_short(s, a, st, ev0, ev1);
   const dim3 grid(wgs), block(split ? 2 * kTreeThreads : kTreeThreads);
-#define LAUNCH_TREE(DD)                                                                               \
-  (split ? hipExtLaunchKernelGGL((k_attn_tree<DD, 2>), grid, block, 0, st, ev0, ev1, 0, s, a)          \
-         : hipExtLaunchKernelGGL((k_attn_tree<DD, 1>), grid, block, 0, st, ev0, ev1, 0, s, a))
+#define LAUNCH_TREE_PFX(DD, PFX)                                                                      \
+  (split ? hipExtLaunchKernelGGL((k_attn_tree<DD, 2, PFX>), grid, block, 0, st, ev0, ev1, 0, s, a)     \
+         : hipExtLaunchKernelGGL((k_attn_tree<DD, 1, PFX>), grid, block, 0, st, ev0, ev1, 0, s, a))
+#define LAUNCH_TREE(DD) (a.prefix ? LAUNCH_TREE_PFX(DD, true) : LAUNCH_TREE_PFX(DD, false))
   switch (s.D) {
     case 64: LAUNCH_TREE(64); break;
     case 96: LAUNCH_TREE(96); break;
@@ -345,6 +347,7 @@ hipError_t launch_attn_tree(const DevState& s, const AttnArgs& a, long max_keys,
     default: return hipErrorInvalidValue;
   }
 #undef LAUNCH_TREE
+#undef LAUNCH_TREE_PFX
   return hipGetLastError();
 }
 

@@ -52,12 +52,14 @@ struct TreeRow {
   uint64_t mask;
   int hi, dmin, dmax;
 };
+// PFX: beside a shared prefix, the launch's queries are q0 .. q0 + qn - 1 of each trie (else all).
+template <bool PFX>
 __device__ inline TreeRow tree_row(const DevState& s, const AttnArgs& a, const TreeUnit& u, int N, int G,
                                    const uint64_t* maskp, const int32_t* depthp, int wave, int col) {
   TreeRow q;
   q.r = u.rb * kTreeRows + wave * 32 + col;
-  q.owner = q.r / G;
-  const int slot = q.r < a.qmax * G ? a.qslots[(size_t)u.t * a.qmax + q.owner] : -1;
+  q.owner = (PFX ? a.q0 : 0) + q.r / G;
+  const int slot = q.r < (PFX ? a.qn : a.qmax) * G ? a.qslots[(size_t)u.t * a.qmax + q.owner] : -1;
   q.ok = slot >= 0 && slot < N;
   q.mask = 0;
   q.depth = -1;
@@ -128,12 +130,37 @@ __device__ inline bool tree_visible(const DevState& s, const TreeRow& q, int i, 
 }
 
 // A wave writes its own rows, O / l: zero for a row without keys or without a query; a NaN score makes
-// l NaN, and the row with it.
-template <int D>
+// l NaN, and the row with it.  Beside a shared prefix (PFX) the row's records of it (their shift, sum and O,
+// in fp32) are merged in first, split by split: a rescale to the larger shift each.
+template <int D, bool PFX>
 __device__ inline void tree_output(const DevState& s, const AttnArgs& a, const TreeUnit& u, const TreeRow& q, int G, int hh,
-                                   float lsum, const f32x16 (&o)[D / 32]) {
+                                   float m, float lsum, f32x16 (&o)[D / 32]) {
   lsum += __shfl_xor(lsum, 32);
-  if (q.r >= a.qmax * G) return;
+  if (q.r >= (PFX ? a.qn : a.qmax) * G) return;
+  if (PFX && q.ok) {
+    const float* rec = a.prefix + ((((size_t)u.li * s.T + u.t) * a.qn + (q.owner - a.q0)) * s.Hq + u.g * G + q.r % G) *
+                                      a.prefix_splits * (D + 2);
+    for (int sp = 0; sp < a.prefix_splits; ++sp, rec += D + 2) {
+      const float m1 = rec[D], l1 = rec[D + 1];
+      if (l1 == 0.0f) continue;  // (no key of the split)
+      const float mn = fmaxf(m, m1);
+      const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(m1 - mn);
+      m = mn;
+      lsum = lsum * f0 + l1 * f1;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          // (records are D + 2 floats: 8-byte aligned)
+          const float2* r2 = reinterpret_cast<const float2*>(rec + 32 * dt + 8 * q4 + 4 * hh);
+          const float2 x = r2[0], y = r2[1];
+          o[dt][4 * q4] = o[dt][4 * q4] * f0 + x.x * f1;
+          o[dt][4 * q4 + 1] = o[dt][4 * q4 + 1] * f0 + x.y * f1;
+          o[dt][4 * q4 + 2] = o[dt][4 * q4 + 2] * f0 + y.x * f1;
+          o[dt][4 * q4 + 3] = o[dt][4 * q4 + 3] * f0 + y.y * f1;
+        }
+    }
+  }
   const bool some = q.ok && lsum != 0.0f;
   const float inv = some ? 1.0f / lsum : 0.0f;
   __bf16* orow = static_cast<__bf16*>(a.out) +

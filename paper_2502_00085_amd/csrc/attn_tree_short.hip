@@ -24,7 +24,7 @@ struct TreeCfg : TreeGeom<D> {
   static_assert(TILE % (16 * kTreeThreads) == 0, "a tile is a whole number of WG loads");
 };
 
-template <int D>
+template <int D, bool PFX>
 __global__ __launch_bounds__(kTreeThreads, 2) void k_attn_tree_short(DevState s, AttnArgs a) {
   using C = TreeCfg<D>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[2 * C::TILE];
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void k_attn_tree_short(DevState s,
   const uint64_t* maskp = s.mask + (size_t)u.t * s.cap + base;
   const int32_t* depthp = s.depth + (size_t)u.t * s.cap + base;
 
-  const TreeRow q = tree_row(s, a, u, N, G, maskp, depthp, wave, col);
+  const TreeRow q = tree_row<PFX>(s, a, u, N, G, maskp, depthp, wave, col);
   const bool any_dead = __ballot(!q.ok) != 0ull;
   const int2 range = tree_range(s, u, q, base, N, lane, wave, wred);
   const int lo = range.x, hi = range.y;
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void k_attn_tree_short(DevState s,
     }
   }
 
-  tree_output<D>(s, a, u, q, G, hh, lsum, o);
+  tree_output<D, PFX>(s, a, u, q, G, hh, m, lsum, o);
 }
 
 }  // namespace
@@ -208,12 +208,16 @@ __global__ __launch_bounds__(kTreeThreads, 2) void k_attn_tree_short(DevState s,
 hipError_t launch_attn_tree_short(const DevState& s, const AttnArgs& a, hipStream_t st, hipEvent_t ev0,
                                   hipEvent_t ev1) {
   const dim3 grid(s.T * a.n_layers * s.Hkv * a.row_blocks), block(kTreeThreads);
+#define LAUNCH_SHORT(DD)                                                                                        \
+  (a.prefix ? hipExtLaunchKernelGGL((k_attn_tree_short<DD, true>), grid, block, 0, st, ev0, ev1, 0, s, a)       \
+            : hipExtLaunchKernelGGL((k_attn_tree_short<DD, false>), grid, block, 0, st, ev0, ev1, 0, s, a))
   switch (s.D) {
-    case 64: hipExtLaunchKernelGGL(k_attn_tree_short<64>, grid, block, 0, st, ev0, ev1, 0, s, a); break;
-    case 96: hipExtLaunchKernelGGL(k_attn_tree_short<96>, grid, block, 0, st, ev0, ev1, 0, s, a); break;
-    case 128: hipExtLaunchKernelGGL(k_attn_tree_short<128>, grid, block, 0, st, ev0, ev1, 0, s, a); break;
+    case 64: LAUNCH_SHORT(64); break;
+    case 96: LAUNCH_SHORT(96); break;
+    case 128: LAUNCH_SHORT(128); break;
     default: return hipErrorInvalidValue;
   }
+#undef LAUNCH_SHORT
   return hipGetLastError();
 }
 

@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kValuThreads) void k_attn_valu(DevState s, AttnArgs
       L += sl[w][i] * f;
       O += so[w][i][c] * f;
     }
-    if (a.splits == 1) {
+    if (!a.partial) {
       const int r = u.rb * R + i;
       if (r < s.b * G) {
         const int bm = r / G, hl = r % G;

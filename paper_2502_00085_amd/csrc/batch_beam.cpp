@@ -255,6 +255,7 @@ td_status batch_beam_attn_decode(bbs_ctx* c, int32_t layer_begin, int32_t n_laye
   a.splits = sp.splits;
   const long units = (long)s.T * n_layers * s.Hkv * a.row_blocks;
   if (units * a.splits > s.attn_pairs_max && a.splits > 1) a.splits = 1;
+  a.partial = a.splits > 1;
   a.xcd_group = 0;
   a.half_wgs = a.splits > 1 && sp.half_wgs;
   hipError_t e = td::launch_attn(kernel, s, a, st, nullptr, nullptr);

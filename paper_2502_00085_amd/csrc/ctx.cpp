@@ -9,49 +9,18 @@
 #include <utility>
 #include <vector>
 
-#include "node_bound.h"
-#include "td_internal.h"
+#include "ctx.h"
 
-struct td_ctx {
-  td_desc desc;
-  td::DevState dev;
-  int device = 0;
-  std::vector<uint8_t> inited;         // per trie: initialised by init_prompt / load_state
-  bool pending = false;                // leaves' K/V rows not yet stored in the pools
-  std::vector<uint8_t> layer_written;  // per layer, while pending
-  bool moves_pending = false;          // rows moved by the last compaction not yet copied
-                                       //   (for the layers not yet written)
-  std::vector<int32_t> leaf_depth;     // per trie: depth of its live leaves (mirrors the
-                                       //   device header; tells which appends collect)
-  std::vector<td::NodeBound> start;    // per trie: its size when it was initialised or loaded
-  int splits_override = 0;             // TD_ATTN_SPLITS (tuning): WGs per attention unit
-  hipEvent_t ev[4][2] = {};             // td_set_kernel_events: per td_phase, the
-                                       //   kernel-timestamp events of its next run
-  std::vector<void*> allocs;
-  std::string err;
-};
+using td::aligned16;
+using td::check_ready;
+using td::fail;
+using td::hip_fail;
 
 namespace {
 
 thread_local std::string g_create_err;
 
 constexpr long kOneRoundWgs = 256;  // attention WGs that run at once (one per CU)
-
-td_status fail(td_ctx* c, td_status st, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  if (c) c->err = buf; else g_create_err = buf;
-  return st;
-}
-
-td_status hip_fail(td_ctx* c, hipError_t e, const char* what) {
-  return fail(c, TD_EHIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 template <typename T>
 hipError_t alloc(td_ctx* c, T** p, size_t n) {
@@ -63,14 +32,6 @@ hipError_t alloc(td_ctx* c, T** p, size_t n) {
   e = hipMemset(q, 0, bytes);
   *p = static_cast<T*>(q);
   return e;
-}
-
-td_status check_ready(td_ctx* c) {
-  if (!c) return TD_EINVAL;
-  c->err.clear();
-  for (size_t t = 0; t < c->inited.size(); ++t)
-    if (!c->inited[t]) return fail(c, TD_ESTATE, "trie %zu is not initialised", t);
-  return TD_OK;
 }
 
 td::TrieShape shape_of(const td::DevState& s) { return {s.b, s.W, s.G, s.cap}; }
@@ -108,7 +69,155 @@ namespace td {
 // The message td_error_string(NULL) returns: a failed td_create, or a failed call that
 // has no context (beam_topk_static).
 void set_error_without_context(const char* msg) { g_create_err = msg; }
+
+td_status fail(td_ctx* c, td_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  if (c) c->err = buf; else g_create_err = buf;
+  return st;
+}
+
+td_status hip_fail(td_ctx* c, hipError_t e, const char* what) {
+  return fail(c, TD_EHIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+td_status check_ready(td_ctx* c) {
+  if (!c) return TD_EINVAL;
+  c->err.clear();
+  for (size_t t = 0; t < c->inited.size(); ++t)
+    if (!c->inited[t]) return fail(c, TD_ESTATE, "trie %zu is not initialised", t);
+  return TD_OK;
+}
+
+void note_written(td_ctx* c, int layer_begin, int n_layers) {
+  if (!c->pending) return;
+  for (int l = layer_begin; l < layer_begin + n_layers; ++l) c->layer_written[l] = 1;
+  bool all = true;
+  for (int l = 0; l < c->dev.L; ++l) all = all && c->layer_written[l];
+  if (all) c->pending = c->moves_pending = false;
+}
+
+// Ranges of layers whose moved rows are due.
+static std::vector<std::pair<int, int>> due_ranges(const td_ctx* c, int layer_begin, int n_layers) {
+  std::vector<std::pair<int, int>> due;
+  if (!c->pending || !c->moves_pending) return due;
+  for (int l = layer_begin; l < layer_begin + n_layers;) {
+    if (c->layer_written[l]) {
+      ++l;
+      continue;
+    }
+    int j = l;
+    while (j < layer_begin + n_layers && !c->layer_written[j]) ++j;
+    due.emplace_back(l, j - l);
+    l = j;
+  }
+  return due;
+}
+
+hipError_t copy_due_rows(td_ctx* c, int layer_begin, int n_layers, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
+  const auto due = due_ranges(c, layer_begin, n_layers);
+  hipError_t e = hipSuccess;
+  for (size_t i = 0; i < due.size(); ++i)
+    if (e == hipSuccess)
+      e = launch_move_rows(c->dev, due[i].first, due[i].second, st, i == 0 ? ev0 : nullptr,
+                           i + 1 == due.size() ? ev1 : nullptr);
+  if (ev0 && due.empty()) {
+    if (e == hipSuccess) e = hipEventRecord(ev0, st);
+    if (e == hipSuccess) e = hipEventRecord(ev1, st);
+  }
+  return e;
+}
 }  // namespace td
+
+namespace {
+
+// The context's device state, with the workspace of the tries' partials beside a prefix pass.
+td::DevState prefix_state(const td_ctx* c) {
+  td::DevState s = c->dev;
+  s.attn_part = c->prefix_trie_part;
+  s.attn_pairs_max = (int)(c->prefix_trie_floats / (32 * (size_t)(s.D + 2)));
+  return s;
+}
+
+// Layers of one launch beside a prefix pass: `rows` query rows (owners of them per trie) of a KV head.
+int prefix_layers(const td_ctx* c, int n_layers, int owners, int rows) {
+  const td::DevState& s = c->dev;
+  const size_t rec = s.D + 2, padded = (size_t)(rows + 31) / 32 * 32;
+  const size_t fit = std::min(c->prefix_floats / ((size_t)s.T * owners * s.Hq * rec),
+                              c->prefix_trie_floats / ((size_t)s.T * s.Hkv * padded * rec));
+  return (int)std::max<size_t>(1, std::min<size_t>(n_layers, fit));
+}
+
+// The launches of trie_attn_decode for layers [layer_begin, +n_layers).
+hipError_t attn_layers(td_ctx* c, int layer_begin, int n_layers, const void* d_q, const void* d_k_new, const void* d_v_new,
+                       void* d_out, float scale_log2, bool rows_copied, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1,
+                       hipEvent_t mv0, hipEvent_t mv1) {
+  const td::DevState s = c->prefix_length > 0 ? prefix_state(c) : c->dev;
+  const long nodes = max_nodes(c, capturing(st));
+  const td::AttnKernel kernel = td::attn_kernel(s, c->desc.attn_impl, n_layers, nodes);
+  const bool mfma = kernel == td::AttnKernel::kMfma;
+  td::AttnArgs a{};
+  a.q = d_q;
+  a.k_new = d_k_new;
+  a.v_new = d_v_new;
+  a.out = d_out;
+  a.layer_begin = layer_begin;
+  a.n_layers = n_layers;
+  a.scale_log2 = scale_log2;
+  a.kv_pending = d_k_new != nullptr ? 1 : 0;
+  const int rpb = td::attn_rows_per_block(s, kernel);
+  a.row_blocks = (s.b * (s.Hq / s.Hkv) + rpb - 1) / rpb;
+  a.row_blocks32 = a.row_blocks;
+  if (mfma && a.row_blocks == 2) {  // b G in (32, 64]: one WG over both row blocks
+    a.rb_per_wg = 2;
+    a.row_blocks = 1;
+  }
+  const td::AttnSplits sp = td::attn_splits(kernel, s, n_layers, a.row_blocks, a.row_blocks32, nodes);
+  a.splits = c->splits_override > 0 ? c->splits_override : sp.splits;
+  a.all_splits = c->splits_override > 0 ? 1 : 0;
+  const long units = (long)s.T * n_layers * s.Hkv * a.row_blocks32;  // (partials per 32-row block)
+  if (units * a.splits > s.attn_pairs_max && a.splits > 1) a.splits = 1;
+  a.xcd_group = a.row_blocks > 1 && ((long)s.T * n_layers * s.Hkv * a.splits) % 8 == 0 ? 1 : 0;
+  // Rows moved by the last compaction are copied before the layer's first attention: by
+  // the attention WGs themselves when each owns a whole (layer, KV head) and every layer
+  // of the call is still due (unless the copy is being timed), else by a copy launch per
+  // due layer range.  The two-row-block kernel has room to stage only a few moved rows
+  // with its first tile; more are copied by each WG after its output, a latency that a
+  // launch of several WG rounds pays once per round on every CU.  There the copy launch
+  // is cheaper (measured with 16 tries of 16 beams at the Llama shape, 31 moved rows per
+  // trie on average: 32 us for the launch against about 140 us inside the attention).
+  const long attn_wgs = (long)s.T * n_layers * s.Hkv * a.row_blocks * a.splits;
+  const bool fuse_moves = a.rb_per_wg == 1 || attn_wgs <= kOneRoundWgs;
+  // (an unsplit launch of several WG rounds, one WG per unit, runs 4-wave WGs, two per CU:
+  // one WG's prologue and merge overlap the other's tile stream)
+  a.half_wgs = a.splits > 1 ? c->splits_override == 0 && sp.half_wgs
+                            : mfma && a.row_blocks == 1 && attn_wgs > kOneRoundWgs;
+  a.moves = 0;
+  const auto due = rows_copied ? std::vector<std::pair<int, int>>() : td::due_ranges(c, layer_begin, n_layers);
+  if (due.size() == 1 && due[0].second == n_layers && a.splits == 1 && a.row_blocks == 1 && !mv0 && fuse_moves)
+    a.moves = 1;
+  hipError_t e = hipSuccess;
+  if (!a.moves && !rows_copied) e = td::copy_due_rows(c, layer_begin, n_layers, st, mv0, mv1);
+  const bool prefix = c->prefix_length > 0;
+  int prefix_splits = 0;
+  if (e == hipSuccess && prefix)
+    e = td::prefix_pass(c, false, layer_begin, n_layers, 0, s.b, s.b, nullptr, d_q, scale_log2, 64, st, ev0, &prefix_splits);
+  a.partial = a.splits > 1 || prefix;
+  if (e == hipSuccess) e = td::launch_attn(kernel, s, a, st, prefix ? nullptr : ev0, a.partial ? nullptr : ev1);
+  if (e == hipSuccess && prefix) {
+    e = td::prefix_merge(c, false, a, prefix_splits, rpb, s.b, st, ev1);
+  } else if (e == hipSuccess && a.splits > 1) {
+    td::AttnArgs ac = a;  // the combine runs per 32-row block
+    ac.row_blocks = a.row_blocks32;
+    e = td::launch_attn_combine(s, ac, rpb, st, nullptr, ev1);
+  }
+  return e;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -197,7 +306,7 @@ td_status td_create(const td_desc* d, td_ctx** out) {
       (e = alloc(c, &s.token, tc)) != hipSuccess || (e = alloc(c, &s.depth, tc)) != hipSuccess ||
       (e = alloc(c, &s.mask, tc)) != hipSuccess ||
       (e = alloc(c, &s.leaf_score, (size_t)s.T * s.b)) != hipSuccess ||
-      (e = alloc(c, &s.status, 2)) != hipSuccess ||
+      (e = alloc(c, &s.status, 2)) != hipSuccess || (e = alloc(c, &s.prefix, 1)) != hipSuccess ||
       (e = alloc(c, &s.lse_part, (size_t)s.T * s.b * s.lse_chunks * 2)) != hipSuccess ||
       (e = alloc(c, &s.topk_keys, 2 * (size_t)s.T * s.b * s.lse_chunks * 16)) != hipSuccess ||
       (e = alloc(c, &s.newpos, tc)) != hipSuccess || (e = alloc(c, &s.moves, tc)) != hipSuccess ||
@@ -266,98 +375,35 @@ td_status trie_attn_decode(td_ctx* c, int32_t layer_begin, int32_t n_layers, con
     return fail(c, TD_EINVAL, "layer range [%d, %d) outside [0, %d)", layer_begin, layer_begin + n_layers, s.L);
   if (!d_q || !d_out || !aligned16(d_q) || !aligned16(d_out))
     return fail(c, TD_EINVAL, "q / out must be non-null and 16-byte aligned");
-  if (c->pending && (!d_k_new || !d_v_new))
+  bool stored = true;  // (by trie_store_kv, for every layer of the call)
+  for (int l = layer_begin; l < layer_begin + n_layers; ++l) stored = stored && (!c->pending || c->layer_written[l]);
+  if (!stored && (!d_k_new || !d_v_new))
     return fail(c, TD_EINVAL, "the leaves' K/V are pending: k_new and v_new are required");
   if (!c->pending && (d_k_new || d_v_new))
     return fail(c, TD_EINVAL, "no leaf K/V is pending (after init/load): pass NULL k_new / v_new");
+  if ((d_k_new == nullptr) != (d_v_new == nullptr)) return fail(c, TD_EINVAL, "pass both k_new and v_new, or neither");
   if (c->pending && (!aligned16(d_k_new) || !aligned16(d_v_new)))
     return fail(c, TD_EINVAL, "k_new / v_new must be 16-byte aligned");
   if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(c, TD_EINVAL, "scale must be finite and > 0");
-  const long nodes = max_nodes(c, capturing(st));
-  const td::AttnKernel kernel = td::attn_kernel(s, c->desc.attn_impl, n_layers, nodes);
-  const bool mfma = kernel == td::AttnKernel::kMfma;
-  td::AttnArgs a{};
-  a.q = d_q;
-  a.k_new = d_k_new;
-  a.v_new = d_v_new;
-  a.out = d_out;
-  a.layer_begin = layer_begin;
-  a.n_layers = n_layers;
-  a.scale_log2 = scale * 1.4426950408889634f;
-  a.kv_pending = c->pending ? 1 : 0;
-  const int rpb = td::attn_rows_per_block(s, kernel);
-  a.row_blocks = (s.b * (s.Hq / s.Hkv) + rpb - 1) / rpb;
-  a.row_blocks32 = a.row_blocks;
-  if (mfma && a.row_blocks == 2) {  // b G in (32, 64]: one WG over both row blocks
-    a.rb_per_wg = 2;
-    a.row_blocks = 1;
-  }
-  const td::AttnSplits sp = td::attn_splits(kernel, s, n_layers, a.row_blocks, a.row_blocks32, nodes);
-  a.splits = c->splits_override > 0 ? c->splits_override : sp.splits;
-  a.all_splits = c->splits_override > 0 ? 1 : 0;
-  const long units = (long)s.T * n_layers * s.Hkv * a.row_blocks32;  // (partials per 32-row block)
-  if (units * a.splits > s.attn_pairs_max && a.splits > 1) a.splits = 1;
-  a.xcd_group = a.row_blocks > 1 && ((long)s.T * n_layers * s.Hkv * a.splits) % 8 == 0 ? 1 : 0;
   hipEvent_t ev0 = c->ev[TD_PHASE_ATTN][0], ev1 = c->ev[TD_PHASE_ATTN][1];
   hipEvent_t mv0 = c->ev[TD_PHASE_MOVES][0], mv1 = c->ev[TD_PHASE_MOVES][1];
   c->ev[TD_PHASE_ATTN][0] = c->ev[TD_PHASE_ATTN][1] = nullptr;
   c->ev[TD_PHASE_MOVES][0] = c->ev[TD_PHASE_MOVES][1] = nullptr;
-  // Rows moved by the last compaction are copied before the layer's first attention: by
-  // the attention WGs themselves when each owns a whole (layer, KV head) and every layer
-  // of the call is still due (unless the copy is being timed), else by a copy launch per
-  // due layer range.  The two-row-block kernel has room to stage only a few moved rows
-  // with its first tile; more are copied by each WG after its output, a latency that a
-  // launch of several WG rounds pays once per round on every CU.  There the copy launch
-  // is cheaper (measured with 16 tries of 16 beams at the Llama shape, 31 moved rows per
-  // trie on average: 32 us for the launch against about 140 us inside the attention).
-  const long attn_wgs = (long)s.T * n_layers * s.Hkv * a.row_blocks * a.splits;
-  const bool fuse_moves = a.rb_per_wg == 1 || attn_wgs <= kOneRoundWgs;
-  // (an unsplit launch of several WG rounds, one WG per unit, runs 4-wave WGs, two per CU:
-  // one WG's prologue and merge overlap the other's tile stream)
-  a.half_wgs = a.splits > 1 ? c->splits_override == 0 && sp.half_wgs
-                            : mfma && a.row_blocks == 1 && attn_wgs > kOneRoundWgs;
-  a.moves = 0;
-  std::vector<std::pair<int, int>> due;
-  if (c->pending && c->moves_pending) {
-    for (int l = layer_begin; l < layer_begin + n_layers;) {
-      if (c->layer_written[l]) {
-        ++l;
-        continue;
-      }
-      int j = l;
-      while (j < layer_begin + n_layers && !c->layer_written[j]) ++j;
-      due.emplace_back(l, j - l);
-      l = j;
-    }
-    if (due.size() == 1 && due[0].second == n_layers && a.splits == 1 && a.row_blocks == 1 && !mv0 &&
-        fuse_moves) {
-      a.moves = 1;
-      due.clear();
-    }
-  }
-  hipEvent_t main_ev1 = a.splits > 1 ? nullptr : ev1;
+  // (with a shared prefix: as many layers per launch as the workspaces of its pass hold)
+  const int chunk = c->prefix_length > 0 ? prefix_layers(c, n_layers, s.b, s.b * (s.Hq / s.Hkv)) : n_layers;
   hipError_t e = hipSuccess;
-  for (size_t i = 0; i < due.size(); ++i)
-    if (e == hipSuccess)
-      e = td::launch_move_rows(s, due[i].first, due[i].second, st, i == 0 ? mv0 : nullptr,
-                               i + 1 == due.size() ? mv1 : nullptr);
-  if (mv0 && due.empty()) {
-    if (e == hipSuccess) e = hipEventRecord(mv0, st);
-    if (e == hipSuccess) e = hipEventRecord(mv1, st);
-  }
-  if (e == hipSuccess) e = td::launch_attn(kernel, s, a, st, ev0, main_ev1);
-  if (e == hipSuccess && a.splits > 1) {
-    td::AttnArgs ac = a;  // the combine runs per 32-row block
-    ac.row_blocks = a.row_blocks32;
-    e = td::launch_attn_combine(s, ac, rpb, st, nullptr, ev1);
+  if (chunk < n_layers) e = td::copy_due_rows(c, layer_begin, n_layers, st, mv0, mv1);
+  const size_t esz = s.dtype == TD_F32 ? 4 : 2;
+  const size_t q_layer = (size_t)s.T * s.b * s.Hq * s.D * esz, kv_layer = (size_t)s.T * s.b * s.Hkv * s.D * esz;
+  auto at = [](const void* p, size_t bytes) { return p ? static_cast<const char*>(p) + bytes : nullptr; };
+  for (int l = 0; l < n_layers && e == hipSuccess; l += chunk) {
+    const int n = std::min(chunk, n_layers - l);
+    e = attn_layers(c, layer_begin + l, n, at(d_q, l * q_layer), at(d_k_new, l * kv_layer), at(d_v_new, l * kv_layer),
+                    static_cast<char*>(d_out) + l * q_layer, scale * 1.4426950408889634f, chunk < n_layers, st,
+                    l == 0 ? ev0 : nullptr, l + n == n_layers ? ev1 : nullptr, mv0, mv1);
   }
   if (e != hipSuccess) return hip_fail(c, e, "trie_attn_decode launch");
-  if (c->pending) {
-    for (int l = layer_begin; l < layer_begin + n_layers; ++l) c->layer_written[l] = 1;
-    bool all = true;
-    for (int l = 0; l < s.L; ++l) all = all && c->layer_written[l];
-    if (all) c->pending = c->moves_pending = false;
-  }
+  td::note_written(c, layer_begin, n_layers);
   return TD_OK;
 }
 
@@ -376,44 +422,82 @@ td_status trie_tree_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32
     return fail(c, TD_EUNSUPPORTED, "tree attention runs on the matrix-core kernels (bf16, head_dim 64, 96 or 128)");
   if (c->pending) return fail(c, TD_ESTATE, "the leaves' K/V are pending: run trie_attn_decode first");
   td::AttnArgs a{};
-  a.q = d_q;
-  a.out = d_out;
-  a.layer_begin = layer_begin;
-  a.n_layers = n_layers;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.tree = 1;
   a.qslots = d_qslots;
   a.qmax = q_max;
+  const bool prefix = c->prefix_length > 0;
+  const size_t layer_bytes = (size_t)s.T * q_max * s.Hq * s.D * 2;
+  auto layers = [&](int l, int n) {
+    a.q = static_cast<const char*>(d_q) + l * layer_bytes;
+    a.out = static_cast<char*>(d_out) + l * layer_bytes;
+    a.layer_begin = layer_begin + l;
+    a.n_layers = n;
+  };
   hipEvent_t ev0 = c->ev[TD_PHASE_ATTN][0], ev1 = c->ev[TD_PHASE_ATTN][1];
-  const long rows = (long)q_max * (s.Hq / s.Hkv);
+  c->ev[TD_PHASE_ATTN][0] = c->ev[TD_PHASE_ATTN][1] = nullptr;
+  const int G = s.Hq / s.Hkv;
+  const long rows = (long)q_max * G;
+  hipError_t e = hipSuccess;
   if (rows >= td::attn_tree_rows_per_block()) {
     // at least one full block of query rows: the prefill-shaped kernel (128 rows per WG,
-    // the key range streamed once for all of them)
+    // the key range streamed once for all of them).  With a shared prefix: as many layers, and
+    // where one layer's records exceed the workspace as many queries, per launch as it holds.
     const int tpb = td::attn_tree_rows_per_block();
-    a.row_blocks = (int)((rows + tpb - 1) / tpb);
-    a.splits = 1;
-    a.xcd_group = a.row_blocks > 1 && ((long)s.T * n_layers * s.Hkv) % 8 == 0 ? 1 : 0;
-    c->ev[TD_PHASE_ATTN][0] = c->ev[TD_PHASE_ATTN][1] = nullptr;
-    // (nearly every node a query, and no window that cuts their ranges)
+    const size_t query = (size_t)s.T * s.Hq * (s.D + 2);  // floats of the records of one query per trie
+    const int lc = !prefix ? n_layers : (int)std::max<size_t>(1, std::min<size_t>(n_layers, c->prefix_floats / (query * q_max)));
+    const int qc = !prefix || lc > 1 ? q_max : (int)std::max<size_t>(1, std::min<size_t>(q_max, c->prefix_floats / query));
     const long nodes = max_nodes(c, false);
-    const bool ramp = q_max >= nodes - nodes / 8 && (s.W <= 0 || s.W >= nodes);
-    hipError_t e = td::launch_attn_tree(s, a, max_keys(c, tpb / (s.Hq / s.Hkv) + 1), ramp, st, ev0, ev1);
+    // (nearly every node a query, and no window that cuts their ranges)
+    const bool ramp = qc >= nodes - nodes / 8 && (s.W <= 0 || s.W >= nodes);
+    a.splits = 1;
+    for (int l = 0; l < n_layers && e == hipSuccess; l += lc) {
+      layers(l, std::min(lc, n_layers - l));
+      for (int q0 = 0; q0 < q_max && e == hipSuccess; q0 += qc) {
+        a.q0 = q0;
+        a.qn = std::min(qc, q_max - q0);
+        a.row_blocks = (int)(((long)a.qn * G + tpb - 1) / tpb);
+        a.xcd_group = a.row_blocks > 1 && ((long)s.T * a.n_layers * s.Hkv) % 8 == 0 ? 1 : 0;
+        hipEvent_t first = l == 0 && q0 == 0 ? ev0 : nullptr;
+        if (prefix) {
+          // (few splits: every row merges their records by itself, one after the other)
+          e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, q0, a.qn, q_max, d_qslots, a.q, a.scale_log2, 8, st, first,
+                              &a.prefix_splits);
+          a.prefix = c->prefix_part;
+          first = nullptr;
+        }
+        if (e == hipSuccess)
+          e = td::launch_attn_tree(s, a, max_keys(c, tpb / G + 1), ramp, st, first,
+                                   l + lc >= n_layers && q0 + qc >= q_max ? ev1 : nullptr);
+      }
+    }
     if (e != hipSuccess) return hip_fail(c, e, "trie_tree_attn launch");
     return TD_OK;
   }
+  const td::DevState ds = prefix ? prefix_state(c) : s;
   const int rpb = td::attn_mfma_rows_per_block();
-  a.row_blocks = (q_max * (s.Hq / s.Hkv) + rpb - 1) / rpb;
+  a.row_blocks = ((int)rows + rpb - 1) / rpb;
   a.row_blocks32 = a.row_blocks;
-  const td::AttnSplits sp = td::attn_mfma_splits(s, n_layers, a.row_blocks, a.row_blocks, max_nodes(c, capturing(st)), true);
-  a.splits = c->splits_override > 0 ? c->splits_override : sp.splits;
-  a.all_splits = c->splits_override > 0 ? 1 : 0;
-  const long units = (long)s.T * n_layers * s.Hkv * a.row_blocks;
-  if (units * a.splits > s.attn_pairs_max && a.splits > 1) a.splits = 1;
-  a.half_wgs = a.splits > 1 && c->splits_override == 0 && sp.half_wgs;
-  a.xcd_group = a.row_blocks > 1 && ((long)s.T * n_layers * s.Hkv * a.splits) % 8 == 0 ? 1 : 0;
-  c->ev[TD_PHASE_ATTN][0] = c->ev[TD_PHASE_ATTN][1] = nullptr;
-  hipError_t e = td::launch_attn_mfma(s, a, st, ev0, a.splits > 1 ? nullptr : ev1);
-  if (e == hipSuccess && a.splits > 1) e = td::launch_attn_combine(s, a, rpb, st, nullptr, ev1);
+  const int chunk = prefix ? prefix_layers(c, n_layers, q_max, (int)rows) : n_layers;
+  for (int l = 0; l < n_layers && e == hipSuccess; l += chunk) {
+    layers(l, std::min(chunk, n_layers - l));
+    hipEvent_t first = l == 0 ? ev0 : nullptr, last = l + chunk >= n_layers ? ev1 : nullptr;
+    const td::AttnSplits sp = td::attn_mfma_splits(ds, a.n_layers, a.row_blocks, a.row_blocks, max_nodes(c, capturing(st)), true);
+    a.splits = c->splits_override > 0 ? c->splits_override : sp.splits;
+    a.all_splits = c->splits_override > 0 ? 1 : 0;
+    const long units = (long)s.T * a.n_layers * s.Hkv * a.row_blocks;
+    if (units * a.splits > ds.attn_pairs_max && a.splits > 1) a.splits = 1;
+    a.half_wgs = a.splits > 1 && c->splits_override == 0 && sp.half_wgs;
+    a.xcd_group = a.row_blocks > 1 && ((long)s.T * a.n_layers * s.Hkv * a.splits) % 8 == 0 ? 1 : 0;
+    a.partial = a.splits > 1 || prefix;
+    int prefix_splits = 0;
+    if (prefix)
+      e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, 0, q_max, q_max, d_qslots, a.q, a.scale_log2, 64, st, first,
+                          &prefix_splits);
+    if (e == hipSuccess) e = td::launch_attn_mfma(ds, a, st, prefix ? nullptr : first, a.partial ? nullptr : last);
+    if (e == hipSuccess && prefix) e = td::prefix_merge(c, true, a, prefix_splits, rpb, q_max, st, last);
+    else if (e == hipSuccess && a.splits > 1) e = td::launch_attn_combine(ds, a, rpb, st, nullptr, last);
+  }
   if (e != hipSuccess) return hip_fail(c, e, "trie_tree_attn launch");
   return TD_OK;
 }

@@ -1,0 +1,66 @@
+// The shared prefix: arguments of its attention pass and of the K/V stores, and the launchers.
+#pragma once
+
+#include "td_internal.h"
+
+namespace td {
+
+// Whose rows a prefix pass takes: the live leaves of every trie, stored nodes of every trie, or
+// consecutive positions of the prefix itself (causal).
+enum class PrefixRows { kLeaves, kNodes, kChunk };
+
+// One pass over the prefix.  Row owner o in [0, tries * per_trie) is query q0 + o % per_trie of trie
+// o / per_trie (kChunk: one "trie", whose query j sits at position pos0 + j); a row is a (owner,
+// query head of one KV head) pair.  Each (row, split) leaves a record of D + 2 floats - O, the shift
+// m (log2 domain) and the sum l - at part[((li * owners + o) * Hq + head) * splits + split].
+struct PrefixArgs {
+  const void* q;                    // [n_layers][tries][q_stride][Hq][D]
+  float* part;                      // records, or null: out gets O / l (splits == 1)
+  void* out;                        // as q
+  const int32_t* qslots = nullptr;  // (kNodes) [tries][q_stride]
+  PrefixRows rows;
+  int layer_begin, n_layers;
+  int tries, per_trie, q0, q_stride;
+  int pos0 = 0;                     // (kChunk)
+  float scale_log2;
+  int row_blocks = 1, splits = 1;
+  int xcd_group = 0;                // row blocks of one (layer, KV head, split) on one XCD
+};
+
+// Query rows of a workgroup for a pass of this many rows per KV head.
+int prefix_rows_per_block(const DevState& s, long rows);
+// Splits of the prefix's keys for `units` (layer, KV head, row block) units over `keys` keys, at most
+// `most`.
+int prefix_splits(const DevState& s, long rows, long units, long keys, long most);
+hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1);
+hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
+                           hipEvent_t ev1);
+
+// Merges a pass's records with those of the tries (attention partials of `splits` splits in blocks of
+// block_rows rows, null: none) into out.
+struct PrefixMergeArgs {
+  const float* prefix;
+  int prefix_splits;
+  const float* trie;
+  int trie_splits, block_rows, row_blocks;
+  void* out;
+  PrefixRows rows;
+  int n_layers, tries, per_trie, q0, q_stride;
+};
+hipError_t launch_prefix_merge(const DevState& s, const PrefixMergeArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1);
+
+// Rotated K/V (and queries) into the pools of the tries or the pages of the prefix.
+struct StoreArgs {
+  const void *q, *k, *v;    // rows [n_layers][tries][n], k / v null: only the queries
+  void* q_out;              // null: no queries
+  const float* freq;        // [rotary / 2], null: no rotation
+  const int32_t* qslots;    // (kNodes) [tries][n]
+  PrefixRows rows;
+  int layer_begin, n_layers, tries, n;
+  int pos0;                 // (kChunk)
+  int rotary, interleaved;
+  int64_t q_stride, k_stride, v_stride;  // elements from one row to the next
+};
+hipError_t launch_store(const DevState& s, const StoreArgs& a, hipStream_t st);
+
+}  // namespace td

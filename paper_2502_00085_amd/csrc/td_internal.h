@@ -27,6 +27,19 @@ struct alignas(16) TrieHdr {
 };
 static_assert(sizeof(TrieHdr) == 64, "one 64-byte header per trie");
 
+// The shared prefix as the kernels see it (one per context, in device memory: a captured call reads
+// the prefix that is attached when it is replayed).
+struct alignas(16) PrefixHdr {
+  const void* k = nullptr;         // [n_pages][L][Hkv][2^shift][D]
+  const void* v = nullptr;
+  const int32_t* table = nullptr;  // page of positions i 2^shift ..; padded by kPrefixTablePad entries
+  int32_t length = 0;              // positions that the tries attend to
+  int32_t shift = 0;               // log2 of the page size
+  int32_t room = 0;                // positions that the table has pages for
+  int32_t pad = 0;
+};
+constexpr int kPrefixTablePad = 8;
+
 // Device-side pointers of one context.  Node arrays are [T][cap], indexed by physical slot.
 struct DevState {
   int T, b, cap, V, L, Hq, Hkv, D, W, dtype;
@@ -62,6 +75,7 @@ struct DevState {
   int32_t* n_moves;      // [T]
   float* attn_part;      // split-combine partials
   int lse_chunks, attn_part_floats, attn_pairs_max;
+  PrefixHdr* prefix = nullptr;  // (contexts of tries; no prefix attached: zeros)
 };
 
 // Batch-based beam search baseline (Alg 1): state of the cache reorder.  `req` holds one
@@ -113,6 +127,10 @@ struct AttnArgs {
                                    // grid's row_blocks counts WGs, of rb_per_wg blocks each
   int all_splits = 0;              // (matrix-core kernel) 1: every split WG takes a share of the
                                    // nodes (a forced split count); 0: only as many as needed
+  int partial = 0;                 // 1: the split partials, also of one split (a merge follows)
+  const float* prefix = nullptr;   // (prefill-shaped tree kernels) records of the shared prefix to merge
+  int prefix_splits = 0;           //   (PrefixArgs::part), of queries q0 .. q0 + qn - 1 of each trie,
+  int q0 = 0, qn = 0;              //   which are the launch's queries; null: every query, no prefix
   int half_wgs = 0;                // (matrix-core kernel) 1: 4-wave WGs, two per CU (two row blocks:
                                    // no fused row copy, moves == 0)
 };

@@ -205,3 +205,55 @@ def test_read_probe_checks_its_arguments_on_the_host(buf, nbytes, method, wgs, s
                          None if sink is None else ctypes.c_void_p(sink), None, None, None)
     assert st == B.TD_EINVAL, L.td_status_name(st)
     assert L.td_error_string(None).decode().startswith("td_read_probe")
+
+
+def test_prefix_calls_reject_a_null_context():
+    L = B.lib()
+    assert L.td_set_prefix(None, None) == B.TD_EINVAL
+    assert L.trie_prefix_store(None, 0, 1, 0, 1, None, None, 0, None, 0, None, 0, None, None) == B.TD_EINVAL
+    assert L.trie_store_kv(None, 0, 1, 1, None, None, None, 0, None, 0, None, 0, None, None) == B.TD_EINVAL
+    assert L.trie_prefix_attn(None, 0, 1, 0, 1, None, None, 1.0, None) == B.TD_EINVAL
+
+
+def test_prefix_binding_checks_layouts_before_the_library():
+    """Host tensors, shapes and element types that the calls do not take (no GPU needed: every one is
+    refused before the library is called)."""
+    import torch
+    dims = B.Dims(_desc())
+    cpu = torch.zeros((2, 2, 2, 16, 128), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        B.td_set_prefix(None, dims, cpu, cpu, (0,), 1)
+    with pytest.raises(ValueError):
+        B.td_set_prefix(None, dims, cpu[:, :1], cpu[:, :1], (0,), 1)
+    k = torch.zeros((2, 3, 2, 128), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        B.trie_prefix_store(None, dims, 0, 2, 0, k, k)
+    with pytest.raises(ValueError):
+        B.Rope(torch.zeros(8))
+
+
+def test_row_strides_of_a_fused_projection():
+    """The row distance that the stores take, from tensors on the meta device dressed as device ones."""
+    import torch
+
+    class Dev:
+        def __init__(self, t):
+            self.t = t
+            self.is_cuda, self.dtype, self.shape = True, t.dtype, t.shape
+
+        def stride(self, *a):
+            return self.t.stride(*a)
+
+        def data_ptr(self):
+            return 4096
+
+    bf = torch.bfloat16
+    fused = torch.zeros((2, 3, 5, 40 * 8 + 16), dtype=bf)
+    part = fused[..., 8:8 + 32].unflatten(-1, (4, 8))
+    assert B._rows(Dev(part), bf, (2, 3, 5), 4, 8, "x") == (4096, 336)
+    assert B._rows(Dev(part[:1, :1, :1]), bf, (1, 1, 1), 4, 8, "x") == (4096, 32)
+    assert B._rows(Dev(part[:1]), bf, (1, 3, 5), 4, 8, "x") == (4096, 336)
+    assert B._rows(None, bf, (1,), 4, 8, "x") == (None, 0)
+    for bad in (part[:, :, :4], part.transpose(1, 2), part[..., :4], part[..., ::2, :]):
+        with pytest.raises(ValueError):
+            B._rows(Dev(bad), bf, tuple(bad.shape[:-2]), *bad.shape[-2:], "x")
