@@ -34,45 +34,52 @@ __device__ inline PrefixUnit prefix_unit(const DevState& s, const PrefixArgs& a)
   return u;
 }
 
-// Row r of a KV head: its owner, its query's place in q and out (in rows of Hq D elements), and the
-// keys [lo, hi) it sees (none: a row past the end, an empty query, or a window past the prefix).
+// Row r of a KV head: its owner, its query's place in q and out (in rows of Hq D elements; a row past
+// the end: the first's), and the keys [lo, hi) it sees (none: a row past the end, an empty query, or
+// a window past the prefix).
 struct PrefixRow {
-  int owner, head;
+  uint32_t owner;
+  int head, t, j;
   size_t at;
   bool in;  // r is a row of the pass
   int lo, hi;
 };
-__device__ inline PrefixRow prefix_row(const DevState& s, const PrefixArgs& a, const PrefixHdr& p, int li, int r) {
-  const int G = s.Hq / s.Hkv;
+__device__ inline PrefixRow prefix_row(const DevState& s, const PrefixArgs& a, int li, uint32_t r) {
+  const uint32_t G = s.Hq / s.Hkv;
   PrefixRow q;
   q.owner = r / G;
-  q.head = r % G;
-  q.in = q.owner < a.tries * a.per_trie;
+  q.head = r - q.owner * G;
+  q.in = q.owner < (uint32_t)(a.tries * a.per_trie);
+  const uint32_t o = q.in ? q.owner : 0;
+  q.t = a.tries == 1 ? 0 : o / (uint32_t)a.per_trie;
+  q.j = a.q0 + o - q.t * a.per_trie;
+  q.at = ((size_t)li * a.tries + q.t) * a.q_stride + q.j;
   q.lo = q.hi = 0;
-  const int t = q.in ? q.owner / a.per_trie : 0, j = a.q0 + (q.in ? q.owner % a.per_trie : 0);
-  q.at = ((size_t)li * a.tries + t) * a.q_stride + j;
-  if (!q.in) return q;
-  int pos;
-  if (a.rows == PrefixRows::kChunk) {
-    pos = a.pos0 + j;
-    q.hi = min(pos + 1, p.room);
-  } else if (a.rows == PrefixRows::kLeaves) {
-    const TrieHdr& h = s.hdr[t];
-    if (j >= h.n_live) return q;
-    pos = p.length + h.leaf_depth;
-    q.hi = p.length;
-  } else {
-    const TrieHdr& h = s.hdr[t];
-    const int slot = a.qslots[(size_t)t * a.q_stride + j];
-    if (slot < 0 || slot >= h.n_nodes) return q;
-    const size_t n = (size_t)t * s.cap + h.base + slot;
-    if (s.mask[n] == 0ull) return q;
-    pos = p.length + s.depth[n];
-    q.hi = p.length;
-  }
-  q.lo = s.W > 0 ? max(0, pos - s.W + 1) : 0;
-  if (q.lo >= q.hi) q.lo = q.hi = 0;
   return q;
+}
+__device__ inline void prefix_row_keys(const DevState& s, const PrefixArgs& a, const PrefixHdr& p, PrefixRow& q) {
+  if (!q.in) return;
+  int pos, hi = p.length;
+  if (a.rows == PrefixRows::kChunk) {
+    pos = a.pos0 + q.j;
+    hi = min(pos + 1, p.room);
+  } else {
+    const TrieHdr& h = s.hdr[q.t];
+    if (a.rows == PrefixRows::kLeaves) {
+      if (q.j >= h.n_live) return;
+      pos = p.length + h.leaf_depth;
+    } else {
+      const int slot = a.qslots[(size_t)q.t * a.q_stride + q.j];
+      if (slot < 0 || slot >= h.n_nodes) return;
+      const size_t n = (size_t)q.t * s.cap + h.base + slot;
+      if (s.mask[n] == 0ull) return;
+      pos = p.length + s.depth[n];
+    }
+  }
+  const int lo = s.W > 0 ? max(0, pos - s.W + 1) : 0;
+  if (lo >= hi) return;
+  q.lo = lo;
+  q.hi = hi;
 }
 
 // Over the 32 rows of a wave that see keys: the first and last key any sees, the range all see.
@@ -110,10 +117,104 @@ __device__ inline TilePages tile_pages(const PrefixHdr& h, int tile) {
   return t;
 }
 
-// The record of a row (PrefixArgs::part).
-__device__ inline float* prefix_record(const DevState& s, const PrefixArgs& a, const PrefixUnit& u, const PrefixRow& q) {
-  const size_t row = ((size_t)u.li * a.tries * a.per_trie + q.owner) * s.Hq + u.g * (s.Hq / s.Hkv) + q.head;
-  return a.part + (row * a.splits + u.split) * (s.D + 2);
+// The keys [lo, hi) that some row of rows [r0, r0 + n) of a KV head sees, and [all_lo, all_hi) that all
+// of them see (those that see any), where they are known without asking the tries: causal rows
+// follow one another, and without a window every other row sees the whole prefix.
+__device__ inline bool prefix_range(const DevState& s, const PrefixArgs& a, const PrefixHdr& p, int r0, int n, PrefixSpan* w) {
+  *w = {0, p.length, 0, p.length};
+  if (a.rows != PrefixRows::kChunk) return s.W <= 0;
+  const int G = s.Hq / s.Hkv, first = a.pos0 + a.q0 + r0 / G, last = a.pos0 + a.q0 + min((r0 + n - 1) / G, a.per_trie - 1);
+  w->hi = min(last + 1, p.room);
+  w->all_hi = min(first + 1, p.room);
+  if (s.W > 0) {
+    w->lo = max(0, first - s.W + 1);
+    w->all_lo = max(0, last - s.W + 1);
+  }
+  if (w->lo >= w->hi) *w = {0, 0, 0, 0};
+  return true;
+}
+
+// The same from the rows of RW waves (rw < RW; every thread calls it).
+template <int RW>
+__device__ inline PrefixSpan prefix_range_of(const PrefixSpan& w, int rw, bool writes, int (*red)[RW]) {
+  if (writes) {
+    red[0][rw] = w.lo;
+    red[1][rw] = w.hi;
+    red[2][rw] = w.all_lo;
+    red[3][rw] = w.all_hi;
+  }
+  __syncthreads();
+  PrefixSpan r = {INT_MAX, 0, 0, INT_MAX};
+  for (int i = 0; i < RW; ++i) {
+    r.lo = min(r.lo, red[0][i]);
+    r.hi = max(r.hi, red[1][i]);
+    r.all_lo = max(r.all_lo, red[2][i]);
+    r.all_hi = min(r.all_hi, red[3][i]);
+  }
+  r.lo = __builtin_amdgcn_readfirstlane(r.lo);
+  r.hi = __builtin_amdgcn_readfirstlane(r.hi);
+  r.all_lo = __builtin_amdgcn_readfirstlane(r.all_lo);
+  r.all_hi = __builtin_amdgcn_readfirstlane(r.all_hi);
+  return r;
+}
+
+// A wave's rows go out: 32 rows of O (lane: row col, elements 32 dt + 8 q4 + 4 hh .. + 3), transposed
+// through `buf` (32 D floats of LDS that no other wave uses) so that a row is written in one piece.
+// Rows of the pass only; a record without a key has no O.  T: the type of `out`.
+template <typename T, int D>
+__device__ inline void prefix_output(const DevState& s, const PrefixArgs& a, const PrefixUnit& u, const PrefixRow& q, int lane,
+                                     float m, float lsum, const f32x16 (&o)[D / 32], float* buf) {
+  constexpr int CH = D / 4;  // 16-byte chunks of a row, rotated by the row's number
+  const int col = lane & 31, hh = lane >> 5, G = s.Hq / s.Hkv;
+  const bool some = q.in && q.lo < q.hi && lsum != 0.0f;  // (a NaN sum is a NaN row)
+  const bool record = a.part_o != nullptr;
+  const float f = record ? 1.0f : some ? 1.0f / lsum : 0.0f;
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = record || some ? o[dt][4 * q4 + e] * f : 0.0f;
+      *reinterpret_cast<f32x4*>(buf + col * D + (8 * dt + 2 * q4 + hh + col) % CH * 4) = x;
+    }
+  // where the row goes: its record, or its row of out (-1: nowhere)
+  int64_t at = -1;
+  if (record) {
+    at = (((int64_t)u.li * a.tries * a.per_trie + q.owner) * s.Hq + u.g * G + q.head) * a.splits + u.split;
+    if (q.in && hh == 0) a.part_ml[at] = make_float2(some ? m : kPrefixNegBig, some ? lsum : 0.0f);
+    if (!some) at = -1;
+  } else if (q.in) {
+    at = (int64_t)q.at * s.Hq + u.g * G + q.head;
+  }
+  const int alo = (int)at, ahi = (int)(at >> 32);
+  if (record || sizeof(T) == 4) {
+    float* const dst = record ? a.part_o : reinterpret_cast<float*>(a.out);
+#pragma unroll 4
+    for (int k = 0; k < 32 * CH / 64; ++k) {
+      const int i = 64 * k + lane, row = i / CH, c = i % CH;
+      const int64_t to = ((int64_t)__shfl(ahi, row) << 32) | (uint32_t)__shfl(alo, row);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(buf + row * D + (c + row) % CH * 4);
+      if (to >= 0) *reinterpret_cast<f32x4*>(dst + to * D + 4 * c) = x;
+    }
+  } else {
+    typedef T t8 __attribute__((ext_vector_type(8)));
+#pragma unroll 2
+    for (int k = 0; k < 32 * CH / 128; ++k) {
+      const int i = 64 * k + lane, row = i / (CH / 2), c = i % (CH / 2);
+      const int64_t to = ((int64_t)__shfl(ahi, row) << 32) | (uint32_t)__shfl(alo, row);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(buf + row * D + (2 * c + row) % CH * 4);
+      const f32x4 y = *reinterpret_cast<const f32x4*>(buf + row * D + (2 * c + 1 + row) % CH * 4);
+      t8 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[e] = (T)x[e];
+        w[4 + e] = (T)y[e];
+      }
+      if (to >= 0) *reinterpret_cast<t8*>(static_cast<T*>(a.out) + to * D + 8 * c) = w;
+    }
+  }
 }
 
 }  // namespace td

@@ -32,50 +32,62 @@ struct PrefixCfg {
   static constexpr int CPR = D / 8;        // 16-byte chunks per key row
   static constexpr int NBLK = CPR / 4;     // 64-byte blocks per row
   static constexpr int HALF = 32 * D * 2;  // bytes of 32 K (or V) rows
-  static constexpr int LOADS = 2 * HALF / 16 / THREADS;  // 16-byte loads per thread: K (or V) of a tile
-  static_assert(2 * HALF % (16 * THREADS) == 0, "a tile is a whole number of WG loads");
+  static constexpr int CHUNKS = 2 * HALF / 16;           // of K (or V) of a tile
+  static constexpr int LOADS = (CHUNKS + THREADS - 1) / THREADS;  // 16-byte loads per thread
+  static constexpr bool RAGGED = CHUNKS % THREADS != 0;  // (the last of them by some of the waves)
+  static_assert(CHUNKS % 64 == 0, "a tile is a whole number of wave loads");
   static constexpr bool ONE_OFS = THREADS % CPR == 0 && (THREADS / CPR) % CPR == 0;
   static constexpr int OFS = ONE_OFS ? 1 : LOADS;
-  static constexpr int WAVES = D <= 128 ? 2 : 1;      // per SIMD: as many as the LDS allows
+  static constexpr int WAVES = D <= 128 || THREADS == 512 ? 2 : 1;  // per SIMD, as the LDS allows
   static constexpr int VROT = 8 % NBLK == 0 ? 1 : 4;  // rotations of V rows 8 apart
 };
 
 template <int D, int RW, int KW>
 __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k_attn_prefix(DevState s, PrefixArgs a) {
   using C = PrefixCfg<D, RW, KW>;
-  static_assert(KW == 1 || (KW == 2 && RW <= 2), "the second group's O fits the K buffers");
+  static_assert(KW == 1 || KW == 2, "one or two groups");
   constexpr int NH = 2 / KW;  // 32-key halves of a tile per wave
   // (four arrays, each used for one buffer only: the compiler can tell an operand read of one buffer
   // from the direct loads under way into the other)
   __shared__ __attribute__((aligned(16))) unsigned char kbuf0[2 * C::HALF], vbuf0[2 * C::HALF];
   __shared__ __attribute__((aligned(16))) unsigned char kbuf1[2 * C::HALF], vbuf1[2 * C::HALF];
-  __shared__ int wred[2][RW];
-  const PrefixUnit u = prefix_unit(s, a);
+  __shared__ int wred[4][RW];
+  __shared__ float ml[KW == 2 ? RW * 128 : 1];
   const PrefixHdr p = *s.prefix;
+  const PrefixUnit u = prefix_unit(s, a);
   const int lab = a.layer_begin + u.li;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW;
   const int col = lane & 31, hh = lane >> 5;
 
-  const PrefixRow q = prefix_row(s, a, p, u.li, (u.rb * RW + rw) * 32 + col);
-  const PrefixSpan span = prefix_span(q);
-  if (lane == 0 && kw == 0) {
-    wred[0][rw] = span.lo;
-    wred[1][rw] = span.hi;
+  const int r0 = u.rb * RW * 32;
+  PrefixRow q = prefix_row(s, a, u.li, r0 + rw * 32 + col);
+  // the lane's query row as B operands of S^T: half hh of its d range (loaded before anything is known
+  // of the row; a row that sees nothing has no say)
+  bf16x8 qv[C::KSTEPS];
+  {
+    const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const __bf16*>(a.q) +
+                                                     (q.at * s.Hq + u.g * (s.Hq / s.Hkv) + q.head) * D + hh * (D / 2));
+#pragma unroll
+    for (int k = 0; k < C::KSTEPS; ++k) qv[k] = __builtin_bit_cast(bf16x8, qp[k]);
   }
-  __syncthreads();
-  int lo = INT_MAX, hi = 0;
-  for (int w = 0; w < RW; ++w) {
-    lo = min(lo, wred[0][w]);
-    hi = max(hi, wred[1][w]);
+  PrefixSpan span, all;  // (of the wave; of the WG)
+  const bool known = prefix_range(s, a, p, r0, RW * 32, &all);
+  if (!known) {  // a window: from the rows' positions
+    prefix_row_keys(s, a, p, q);
+    span = prefix_span(q);
+    all = prefix_range_of<RW>(span, rw, lane == 0 && kw == 0, wred);
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
+  const int lo = all.lo, hi = all.hi;
   // tiles of 64 keys, at multiples of 64: this split's share
   const int first = hi > 0 ? lo / 64 : 0, tiles = hi > 0 ? (hi + 63) / 64 - first : 0;
   const int per = (tiles + a.splits - 1) / a.splits;
-  const int t0 = first + u.split * per, t1 = min(first + tiles, t0 + per);
+  const int t0 = first + u.split * per, t1 = max(t0, min(first + tiles, t0 + per));
+  // of it [m0, m1): tiles that every row sees whole; the cut ones before and after
+  const int m0 = min(max(t0, (all.all_lo + 63) / 64), t1), m1 = max(m0, min(t1, all.all_hi / 64));
+  const int before = m0 - t0, cut = before + t1 - m1;
+  auto cut_tile = [&](int i) __attribute__((always_inline)) { return i < before ? t0 + i : m1 + i - before; };
 
   const size_t head = ((size_t)lab * s.Hkv + u.g) << p.shift;  // rows before this (layer, KV head) in a page
   const size_t page_rows = ((size_t)s.L * s.Hkv) << p.shift;
@@ -101,6 +113,7 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     const int last = hi - 1 - tb;  // (rows past the end: the last row)
 #pragma unroll
     for (int j = 0; j < C::LOADS; ++j) {
+      if (C::RAGGED && j * C::THREADS + wave * 64 >= C::CHUNKS) break;
       const uint32_t step = C::ONE_OFS ? j * (C::THREADS / C::CPR) * 2 * D : 0;
       uint32_t ko = kofs[C::ONE_OFS ? 0 : j], vo = vofs[C::ONE_OFS ? 0 : j];
       const unsigned char *ks = kt + step, *vs = vt + step;
@@ -129,14 +142,20 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     }
   };
 
-  // the lane's query row as B operands of S^T: half hh of its d range
-  bf16x8 qv[C::KSTEPS];
-  {
-    const bool some = q.lo < q.hi;
-    const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const __bf16*>(a.q) +
-                                                     ((some ? q.at : 0) * s.Hq + u.g * (s.Hq / s.Hkv) + q.head) * D + hh * (D / 2));
-#pragma unroll
-    for (int k = 0; k < C::KSTEPS; ++k) qv[k] = __builtin_bit_cast(bf16x8, some ? qp[k] : make_uint4(0, 0, 0, 0));
+  // the first two tiles go out before anything that waits for the tries
+  TilePages next{};
+  if (t0 < t1) {
+    const bool main = m0 < m1;
+    const int x0 = main ? m0 : cut_tile(0), x1 = main ? m0 + 1 : cut_tile(1);
+    const bool two = main ? m0 + 1 < m1 : cut > 1;
+    const TilePages pg0 = tile_pages(p, x0), pg1 = tile_pages(p, two ? x1 : x0);
+    issue(x0, pg0, kbuf0, vbuf0);
+    if (two) issue(x1, pg1, kbuf1, vbuf1);
+    if (m0 + 2 < m1) next = tile_pages(p, m0 + 2);
+  }
+  if (known) {
+    prefix_row_keys(s, a, p, q);
+    span = prefix_span(q);
   }
   const int grp = lane >> 4, tm = (lane & 15) >> 2, tq = lane & 3;
   int kread[C::KSTEPS], vread[C::VROT][C::DT];
@@ -167,17 +186,59 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     return __builtin_shufflevector(p0, p1, 0, 1, 2, 3, 4, 5, 6, 7);
   };
 
-  TilePages next;
+  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+  // Probabilities of this lane's 16 keys relative to the row's shift m, rounded to bf16 (the operand
+  // type of the second product; the sum takes the rounded ones, so that an error of a weight is in
+  // numerator and denominator alike), and their sum.  Softmax does not depend on the shift: it moves
+  // only when the probabilities leave their range, which their sum tells.
+  auto weigh = [&](const f32x16& acc, bf16x8 (&pb)[2]) __attribute__((always_inline)) {
+    float ps = 0.0f;
+    auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) pb[v >> 3][v & 7] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(acc[v], scale, -m));
+      ps = 0.0f;
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) {
+        const bf16x2 pair = {pb[v >> 3][v & 7], pb[v >> 3][(v & 7) + 1]};
+        ps = __builtin_amdgcn_fdot2_f32_bf16(pair, ones, ps, false);
+      }
+    };
+    weights();
+    if (__any(ps > kMost)) {
+      float tmax = acc[0];
+#pragma unroll
+      for (int v = 1; v < 16; ++v) tmax = fmaxf(tmax, acc[v]);
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32)) * scale;
+      const float mn = tmax > m + kSlack ? tmax : m;
+      const float alpha = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      lsum *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[dt][v] *= alpha;
+      weights();
+    }
+    lsum += ps;
+  };
+  auto add_values = [&](const unsigned char* vh, const bf16x8 (&pb)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+      for (int dt = 0; dt < C::DT; ++dt)
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vop(vh, uu, dt)), pb[uu], o[dt], 0, 0, 0);
+  };
   auto step = [&](int tile, const unsigned char* kb, const unsigned char* vb, unsigned char* knext,
                   unsigned char* vnext) __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(kWaitVmAll);  // this thread's loads of the tile have landed
-    __syncthreads();                         // every thread's have; the other buffer is free
-    if (tile + 1 < t1) {
+    // this thread's loads of the tile have landed, then every thread's, and the other buffer is free
+    // (the second tile is on its way already)
+    if (!C::RAGGED && tile == m0 && m0 + 1 < m1) __builtin_amdgcn_s_waitcnt(wait_vm(2 * C::LOADS));
+    else __builtin_amdgcn_s_waitcnt(kWaitVmAll);
+    __syncthreads();
+    if (tile > m0 && tile + 1 < m1) {
       issue(tile + 1, next, knext, vnext);
-      if (tile + 2 < t1) next = tile_pages(p, tile + 2);
+      if (tile + 2 < m1) next = tile_pages(p, tile + 2);
     }
-    const int tb = tile * 64;
-    if (tb >= span.hi || tb + 64 <= span.lo) return;  // (wave-uniform) no row sees the tile
     f32x16 acc[NH];
 #pragma unroll
     for (int h = 0; h < NH; ++h)
@@ -189,60 +250,56 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
       for (int h = 0; h < NH; ++h)
         acc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
             *reinterpret_cast<const bf16x8*>(kb + (KW == 2 ? kw : h) * C::HALF + kread[k]), qv[k], acc[h], 0, 0, 0);
-    // a row's interval cuts the tile: hidden scores become -inf
-    const bool cut = tb < span.all_lo || tb + 64 > span.all_hi;
-    if (cut) {
-#pragma unroll
-      for (int h = 0; h < NH; ++h)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int n = tb + 32 * (KW == 2 ? kw : h) + 8 * (v >> 2) + 4 * hh + (v & 3);
-          acc[h][v] = (n >= q.lo) & (n < q.hi) ? acc[h][v] : -INFINITY;
-        }
-    }
-    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
-      const int half = KW == 2 ? kw : h;
-      // Probabilities relative to the row's shift m, rounded to bf16 (the operand type of the second
-      // product; the sum takes the rounded ones, so the rounding errors of numerator and denominator
-      // go together), and their sum over this lane's 16 keys.  Softmax does not depend on the shift:
-      // it moves only when the probabilities leave their range, which their sum tells.
       bf16x8 pb[2];
-      float ps = 0.0f;
-      auto weights = [&]() __attribute__((always_inline)) {
+      weigh(acc[h], pb);
+      add_values(vb + (KW == 2 ? kw : h) * C::HALF, pb);
+    }
+  };
+  for (int t = m0; t < m1; t += 2) {
+    step(t, kbuf0, vbuf0, kbuf1, vbuf1);
+    if (t + 1 < m1) step(t + 1, kbuf1, vbuf1, kbuf0, vbuf0);
+  }
+
+  // the cut tiles, two at a time: the ends of the rows' ranges
+  for (int i = 0; i < cut; i += 2) {
+    if (i > 0 || m0 < m1) {
+      const bool two = i + 1 < cut;
+      const TilePages pg0 = tile_pages(p, cut_tile(i)), pg1 = tile_pages(p, cut_tile(two ? i + 1 : i));
+      __syncthreads();  // both buffers are free
+      issue(cut_tile(i), pg0, kbuf0, vbuf0);
+      if (two) issue(cut_tile(i + 1), pg1, kbuf1, vbuf1);
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitVmAll);
+    __syncthreads();
+    const int halves = 2 * min(2, cut - i);
+#pragma unroll 1
+    for (int h = KW == 2 ? kw : 0; h < halves; h += KW) {
+      const int hb = cut_tile(i + h / 2) * 64 + 32 * (h & 1);
+      if (hb >= span.hi || hb + 32 <= span.lo) continue;  // (wave-uniform) no row sees them
+      const unsigned char* kh = (h < 2 ? kbuf0 : kbuf1) + (h & 1) * C::HALF;
+      const unsigned char* vh = (h < 2 ? vbuf0 : vbuf1) + (h & 1) * C::HALF;
+      f32x16 acc;
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          pb[v >> 3][v & 7] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(acc[h][v], scale, -m));
-        ps = 0.0f;
+      for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
 #pragma unroll
-        for (int v = 0; v < 16; v += 2) {
-          const bf16x2 pair = {pb[v >> 3][v & 7], pb[v >> 3][(v & 7) + 1]};
-          ps = __builtin_amdgcn_fdot2_f32_bf16(pair, ones, ps, false);
+      for (int k = 0; k < C::KSTEPS; ++k)
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kh + kread[k]), qv[k], acc, 0, 0, 0);
+      bf16x8 pb[2];
+      const bool whole = hb >= span.all_lo && hb + 32 <= span.all_hi;  // (wave-uniform)
+      if (!whole) {  // hidden scores become -inf
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int n = hb + 8 * (v >> 2) + 4 * hh + (v & 3);
+          acc[v] = ((n >= q.lo) & (n < q.hi)) ? acc[v] : -INFINITY;
         }
-      };
-      weights();
-      if (__any(ps > kMost)) {
-        float tmax = acc[h][0];
-#pragma unroll
-        for (int v = 1; v < 16; ++v) tmax = fmaxf(tmax, acc[h][v]);
-        tmax = fmaxf(tmax, __shfl_xor(tmax, 32)) * scale;
-        const float mn = tmax > m + kSlack ? tmax : m;
-        const float alpha = __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        lsum *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) o[dt][v] *= alpha;
-        weights();
       }
-      lsum += ps;
-      const unsigned char* vh = vb + half * C::HALF;
-      if (cut) {
-        // A hidden key weighs 0, but 0 times an infinite or NaN V is NaN: a tile that is cut and
-        // holds such a V adds its products key by key, to the rows that see the key.
-        bool odd = false;
+      weigh(acc, pb);
+      // A hidden key weighs 0, but 0 times an infinite or NaN V is NaN: a tile that holds such a V
+      // adds its products key by key, to the rows that see the key.
+      bool odd = false;
+      if (!whole) {
 #pragma unroll
         for (int uu = 0; uu < 2; ++uu)
 #pragma unroll
@@ -251,103 +308,65 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
 #pragma unroll
             for (int e = 0; e < 8; ++e) odd |= (x[e] & 0x7f80) == 0x7f80;
           }
-        if (__any(odd)) {
-#pragma unroll 1
-          for (int i = 0; i < 32; ++i) {  // key tb + 32 half + i, held by half-wave (i / 4) % 2
-            const int n = tb + 32 * half + i, vi = (i >> 3) * 4 + (i & 3);
-            float w = 0.0f;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) w = v == vi ? (float)pb[v >> 3][v & 7] : w;
-            w = __shfl(w, col + 32 * ((i >> 2) & 1));
-            const bool own = n >= q.lo && n < q.hi;
-#pragma unroll
-            for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-              for (int q4 = 0; q4 < 4; ++q4) {
-                // elements 32 dt + 8 q4 + 4 hh .. + 3 of the key's V row
-                const bf16x4 x = *reinterpret_cast<const bf16x4*>(
-                    vh + i * (2 * D) + phys_chunk<C::CPR, C::NBLK>(i, 4 * dt + q4) * 16 + 8 * hh);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[dt][4 * q4 + e] += own ? w * (float)x[e] : 0.0f;
-              }
-          }
-          continue;
-        }
       }
+      if (!__any(odd)) {
+        add_values(vh, pb);
+        continue;
+      }
+#pragma unroll 1
+      for (int n = 0; n < 32; ++n) {  // key hb + n, held by half-wave (n / 4) % 2
+        const int vi = (n >> 3) * 4 + (n & 3);
+        float w = 0.0f;
 #pragma unroll
-      for (int uu = 0; uu < 2; ++uu)
+        for (int v = 0; v < 16; ++v) w = v == vi ? (float)pb[v >> 3][v & 7] : w;
+        w = __shfl(w, col + 32 * ((n >> 2) & 1));
+        const bool own = hb + n >= q.lo && hb + n < q.hi;
 #pragma unroll
         for (int dt = 0; dt < C::DT; ++dt)
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vop(vh, uu, dt)), pb[uu], o[dt], 0, 0, 0);
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            // elements 32 dt + 8 q4 + 4 hh .. + 3 of the key's V row
+            const bf16x4 x = *reinterpret_cast<const bf16x4*>(
+                vh + n * (2 * D) + phys_chunk<C::CPR, C::NBLK>(n, 4 * dt + q4) * 16 + 8 * hh);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[dt][4 * q4 + e] += own ? w * (float)x[e] : 0.0f;
+          }
+      }
     }
-  };
-  if (t0 < t1) {
-    issue(t0, tile_pages(p, t0), kbuf0, vbuf0);
-    if (t0 + 1 < t1) next = tile_pages(p, t0 + 1);
-  }
-  for (int t = t0; t < t1; t += 2) {
-    step(t, kbuf0, vbuf0, kbuf1, vbuf1);
-    if (t + 1 < t1) step(t + 1, kbuf1, vbuf1, kbuf0, vbuf0);
   }
 
   if constexpr (KW == 2) {
-    // the second group hands its state over through LDS, lane by lane
+    // the second group hands its state over through LDS, lane by lane: a quarter of O in each buffer
+    static_assert(RW * 64 * (D / 8) * 4 <= 2 * C::HALF, "a quarter of O fits a buffer");
     __syncthreads();  // every wave has read its last tile
-    float* const o0 = reinterpret_cast<float*>(kbuf0);
-    float* const o1 = reinterpret_cast<float*>(kbuf1);
-    float* const ml = reinterpret_cast<float*>(vbuf0);
+    float* const part[4] = {reinterpret_cast<float*>(kbuf0), reinterpret_cast<float*>(vbuf0), reinterpret_cast<float*>(kbuf1),
+                            reinterpret_cast<float*>(vbuf1)};
     if (kw == 1) {
 #pragma unroll
-      for (int x = 0; x < D / 4; ++x) {
-        const int at = (rw * (D / 4) + x) * 64 + lane, y = x + D / 4;
-        o0[at] = o[x / 16][x % 16];
-        o1[at] = o[y / 16][y % 16];
-      }
+      for (int x = 0; x < D / 2; ++x) part[x / (D / 8)][(rw * (D / 8) + x % (D / 8)) * 64 + lane] = o[x / 16][x % 16];
       ml[rw * 128 + lane] = m;
       ml[rw * 128 + 64 + lane] = lsum;
     }
     __syncthreads();
-    if (kw == 1) return;
-    const float m1 = ml[rw * 128 + lane], l1 = ml[rw * 128 + 64 + lane];
-    const float mn = fmaxf(m, m1);
-    const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(m1 - mn);
-    m = mn;
-    lsum = lsum * f0 + l1 * f1;
+    if (kw == 0) {
+      const float m1 = ml[rw * 128 + lane], l1 = ml[rw * 128 + 64 + lane];
+      const float mn = fmaxf(m, m1);
+      const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(m1 - mn);
+      m = mn;
+      lsum = lsum * f0 + l1 * f1;
 #pragma unroll
-    for (int x = 0; x < D / 4; ++x) {
-      const int at = (rw * (D / 4) + x) * 64 + lane, y = x + D / 4;
-      o[x / 16][x % 16] = o[x / 16][x % 16] * f0 + o0[at] * f1;
-      o[y / 16][y % 16] = o[y / 16][y % 16] * f0 + o1[at] * f1;
+      for (int x = 0; x < D / 2; ++x)
+        o[x / 16][x % 16] = o[x / 16][x % 16] * f0 + part[x / (D / 8)][(rw * (D / 8) + x % (D / 8)) * 64 + lane] * f1;
     }
+    __syncthreads();
+    if (kw == 1) return;
+  } else {
+    __syncthreads();  // every wave has read its last tile
   }
 
   lsum += __shfl_xor(lsum, 32);
-  if (!q.in) return;
-  const bool some = q.lo < q.hi && lsum != 0.0f;  // (a NaN sum is a NaN row)
-  if (a.part != nullptr) {
-    float* rec = prefix_record(s, a, u, q);
-#pragma unroll
-    for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        float2* r2 = reinterpret_cast<float2*>(rec + 32 * dt + 8 * q4 + 4 * hh);
-        r2[0] = make_float2(o[dt][4 * q4], o[dt][4 * q4 + 1]);
-        r2[1] = make_float2(o[dt][4 * q4 + 2], o[dt][4 * q4 + 3]);
-      }
-    if (hh == 0) *reinterpret_cast<float2*>(rec + D) = make_float2(some ? m : kPrefixNegBig, some ? lsum : 0.0f);
-  } else {
-    const float inv = some ? 1.0f / lsum : 0.0f;
-    __bf16* orow = static_cast<__bf16*>(a.out) + (q.at * s.Hq + u.g * (s.Hq / s.Hkv) + q.head) * D;
-#pragma unroll
-    for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        bf16x4 y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = (__bf16)(some ? o[dt][4 * q4 + e] * inv : 0.0f);
-        *reinterpret_cast<bf16x4*>(orow + 32 * dt + 8 * q4 + 4 * hh) = y;
-      }
-  }
+  unsigned char* const mine = rw == 0 ? kbuf0 : rw == 1 ? vbuf0 : rw == 2 ? kbuf1 : vbuf1;
+  prefix_output<__bf16, D>(s, a, u, q, lane, m, lsum, o, reinterpret_cast<float*>(mine));
 }
 
 template <int D>
@@ -358,85 +377,112 @@ void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, h
   else hipExtLaunchKernelGGL((k_attn_prefix<D, 4, 1>), grid, dim3(256), 0, st, ev0, ev1, 0, s, a);
 }
 
-// One wave per (row, merge): lanes hold the row's d in 8-byte pieces.  Every record's shift and sum
-// first, then the weighted O of all of them.
-constexpr int kMergeThreads = 256;
+// Each (row, 8-element chunk of d) is merged by TP adjacent lanes, lane j taking the groups of 8
+// records j, j + TP, ...: every load of a group goes out before any is used; groups are merged with
+// a running shift, the lanes' states pairwise, in one order.  A record with sum 0 weighs nothing
+// (whatever its O); a NaN sum makes the row NaN.
+constexpr int kMergeThreads = 64;
 
-template <typename T>
-__global__ __launch_bounds__(kMergeThreads) void k_prefix_merge(DevState s, PrefixMergeArgs a) {
-  const int D = s.D, G = s.Hq / s.Hkv;
-  const int lane = threadIdx.x & 63;
-  const long rows = (long)a.n_layers * a.tries * a.per_trie * s.Hq;
-  const long row = (long)blockIdx.x * (kMergeThreads / 64) + (threadIdx.x >> 6);
-  if (row >= rows) return;
+template <typename T, int TP>
+__global__ __launch_bounds__(kMergeThreads) void k_prefix_merge(DevState s, PrefixMergeArgs a, uint32_t items) {
+  constexpr int GS = 8;
+  const int D = s.D, G = s.Hq / s.Hkv, CH = D / 8;
+  // (the host keeps items * TP below 2^31)
+  const uint32_t item = (blockIdx.x * kMergeThreads + threadIdx.x) / TP;
+  const int sub = threadIdx.x % TP;
+  if (item >= items) return;  // (the lanes of an item leave together)
+  const uint32_t row = item / CH;
+  const int c = (int)(item % CH) * 8;
   const int head = row % s.Hq;
-  const long o = row / s.Hq;  // (li tries + t) per_trie + j
+  const uint32_t o = row / s.Hq;  // (li tries + t) per_trie + j
   const int j = o % a.per_trie;
-  const int t = (o / a.per_trie) % a.tries, li = (int)(o / a.per_trie / a.tries);
-  const float* prec = a.prefix + row * a.prefix_splits * (D + 2);
+  const uint32_t tl = o / a.per_trie;
+  const int t = tl % a.tries, li = tl / a.tries;
+  const size_t prec = (size_t)row * a.prefix_splits;
+  const int ts = a.trie != nullptr ? a.trie_splits : 0, n = ts + a.prefix_splits;
   const float* trec = nullptr;
   size_t tstep = 0;
-  if (a.trie != nullptr) {
+  if (ts > 0) {
     const int r = j * G + head % G;
     const size_t unit = (((size_t)t * a.n_layers + li) * s.Hkv + head / G) * a.row_blocks + r / a.block_rows;
-    trec = a.trie + (unit * a.trie_splits * a.block_rows + r % a.block_rows) * (D + 2);
+    trec = a.trie + (unit * ts * a.block_rows + r % a.block_rows) * (D + 2);
     tstep = (size_t)a.block_rows * (D + 2);
   }
   const bool live = a.rows != PrefixRows::kLeaves || j < s.hdr[t].n_live;
-  const int n = (a.trie != nullptr ? a.trie_splits : 0) + a.prefix_splits;
-  auto record = [&](int i) {
-    return trec != nullptr && i < a.trie_splits ? trec + i * tstep
-                                                 : prec + (size_t)(i - (trec != nullptr ? a.trie_splits : 0)) * (D + 2);
-  };
-  // lane i: record i, i + 64, ...
-  float m = kPrefixNegBig, l = 0.0f;
-  for (int i = lane; i < n; i += 64) {
-    const float2 ml = *reinterpret_cast<const float2*>(record(i) + D);
-    if (ml.y == 0.0f) continue;
-    const float mn = fmaxf(m, ml.x);
-    l = l * exp2f(m - mn) + ml.y * exp2f(ml.x - mn);
-    m = mn;
-  }
-  float M = m;
-  for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
-  float L = l * exp2f(m - M);
-  for (int x = 32; x > 0; x >>= 1) L += __shfl_xor(L, x);
-  T* out = static_cast<T*>(a.out) + ((((size_t)li * a.tries + t) * a.q_stride + a.q0 + j) * s.Hq + head) * D;
-  const bool some = live && L != 0.0f;
-  for (int c = 2 * lane; c < D; c += 128) {
-    float x = 0.0f, y = 0.0f;
-    if (some) {
-      for (int i = 0; i < n; ++i) {
-        const float* rec = record(i);
-        const float2 ml = *reinterpret_cast<const float2*>(rec + D);
-        if (ml.y == 0.0f) continue;
-        const float f = exp2f(ml.x - M);
-        const float2 v = *reinterpret_cast<const float2*>(rec + c);
-        x += v.x * f;
-        y += v.y * f;
-      }
-      x /= L;
-      y /= L;
+  float M = kPrefixNegBig, L = 0.0f, O[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) O[e] = 0.0f;
+  for (int i0 = sub * GS; i0 < n; i0 += TP * GS) {
+    float2 ml[GS];
+    float2 ov[GS][4];
+#pragma unroll
+    for (int k = 0; k < GS; ++k) {
+      const int i = i0 + k < n ? i0 + k : i0;  // (past the last: the group's first again, unused)
+      // (the tries' records are D + 2 floats, 8-byte aligned)
+      const float* rec = i < ts ? trec + i * tstep : a.prefix_o + (prec + i - ts) * D;
+      ml[k] = i < ts ? *reinterpret_cast<const float2*>(rec + D) : a.prefix_ml[prec + i - ts];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ov[k][e] = *reinterpret_cast<const float2*>(rec + c + 2 * e);
     }
-    typedef T t2 __attribute__((ext_vector_type(2)));
-    t2 w = {(T)x, (T)y};
-    *reinterpret_cast<t2*>(out + c) = w;
+    float Mg = M;
+#pragma unroll
+    for (int k = 0; k < GS; ++k) Mg = i0 + k < n && ml[k].y != 0.0f ? fmaxf(Mg, ml[k].x) : Mg;
+    const float fo = __builtin_amdgcn_exp2f(M - Mg);
+    L *= fo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) O[e] *= fo;
+#pragma unroll
+    for (int k = 0; k < GS; ++k) {
+      const bool use = i0 + k < n && ml[k].y != 0.0f;
+      const float f = __builtin_amdgcn_exp2f(ml[k].x - Mg);
+      L += use ? ml[k].y * f : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        O[2 * e] += use ? ov[k][e].x * f : 0.0f;
+        O[2 * e + 1] += use ? ov[k][e].y * f : 0.0f;
+      }
+    }
+    M = Mg;
   }
+#pragma unroll
+  for (int w = 1; w < TP; w <<= 1) {
+    const float M2 = __shfl_xor(M, w), L2 = __shfl_xor(L, w);
+    float O2[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) O2[e] = __shfl_xor(O[e], w);
+    const bool low = (sub & w) == 0;
+    const float Mn = fmaxf(M, M2);
+    const float f0 = __builtin_amdgcn_exp2f((low ? M : M2) - Mn), f1 = __builtin_amdgcn_exp2f((low ? M2 : M) - Mn);
+    L = (low ? L : L2) * f0 + (low ? L2 : L) * f1;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) O[e] = (low ? O[e] : O2[e]) * f0 + (low ? O2[e] : O[e]) * f1;
+    M = Mn;
+  }
+  if (sub != 0) return;
+  const float inv = live && L != 0.0f ? 1.0f / L : 0.0f;
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  t8 y;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = (T)(live && L != 0.0f ? O[e] * inv : 0.0f);
+  *reinterpret_cast<t8*>(static_cast<T*>(a.out) + ((((size_t)li * a.tries + t) * a.q_stride + a.q0 + j) * s.Hq + head) * D + c) = y;
 }
 
 }  // namespace
 
 int prefix_rows_per_block(const DevState& s, long rows) {
-  if (s.dtype == TD_F32) return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  (void)s;
   return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
 }
 
-int prefix_splits(const DevState& s, long rows, long units, long keys, long most) {
-  (void)s;
-  (void)rows;
+// A WG per CU, of at least 4 tiles of 64 keys; two per CU where each still has 16.  More splits make
+// shorter chains of tiles and more records to merge.  Measured, 8 KV heads at d = 128, the pass and
+// its merge, us: 128 rows over 4,096 keys, 8 / 16 / 32 splits: 22.6 / 20.9 / 24.6; over 16,384 keys, 16 /
+// 32 / 64: 35.1 / 30.5 / 34.1; 1,024 rows (8 blocks) over 1,024 keys, 4 / 8: 25.5 / 27.7; over 8,192 keys,
+// 4 / 8 / 16: 63 / 57 / 72; 32 rows over 4,096 keys, 16 / 32 / 64: 17.4 / 17.9 / 20.1.
+int prefix_splits(long units, long keys, long most) {
   const long tiles = (keys + 63) / 64;
-  const long n = std::min({(512 + units - 1) / units, (tiles + 3) / 4, most, 64l});
-  return (int)std::max(1l, n);
+  const long one = std::min((256 + units - 1) / units, tiles / 4), two = std::min((512 + units - 1) / units, tiles / 16);
+  return (int)std::max(1l, std::min(std::max(one, two), most));
 }
 
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
@@ -453,10 +499,16 @@ hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st,
 }
 
 hipError_t launch_prefix_merge(const DevState& s, const PrefixMergeArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
-  const long rows = (long)a.n_layers * a.tries * a.per_trie * s.Hq;
-  const dim3 grid((rows + kMergeThreads / 64 - 1) / (kMergeThreads / 64));
-  if (s.dtype == TD_F32) hipExtLaunchKernelGGL(k_prefix_merge<float>, grid, dim3(kMergeThreads), 0, st, ev0, ev1, 0, s, a);
-  else hipExtLaunchKernelGGL(k_prefix_merge<__bf16>, grid, dim3(kMergeThreads), 0, st, ev0, ev1, 0, s, a);
+  const long items = (long)a.n_layers * a.tries * a.per_trie * s.Hq * (s.D / 8);
+  const int n = (a.trie ? a.trie_splits : 0) + a.prefix_splits;
+  const int tp = n > 16 ? 4 : n > 8 ? 2 : 1;  // lanes per output chunk: 8 records each
+  if (items * tp >= (1l << 31)) return hipErrorInvalidValue;  // (a workspace of records is far smaller)
+  const dim3 grid((items * tp + kMergeThreads - 1) / kMergeThreads), block(kMergeThreads);
+#define LAUNCH_MERGE(T, TP) \
+  hipExtLaunchKernelGGL((k_prefix_merge<T, TP>), grid, block, 0, st, ev0, ev1, 0, s, a, (uint32_t)items)
+  if (s.dtype == TD_F32) tp == 4 ? LAUNCH_MERGE(float, 4) : tp == 2 ? LAUNCH_MERGE(float, 2) : LAUNCH_MERGE(float, 1);
+  else tp == 4 ? LAUNCH_MERGE(__bf16, 4) : tp == 2 ? LAUNCH_MERGE(__bf16, 2) : LAUNCH_MERGE(__bf16, 1);
+#undef LAUNCH_MERGE
   return hipGetLastError();
 }
 

@@ -44,29 +44,35 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
   using C = Prefix32Cfg<D, RW, KW>;
   __shared__ __attribute__((aligned(16))) unsigned char kbuf0[C::TILE], vbuf0[C::TILE];
   __shared__ __attribute__((aligned(16))) unsigned char kbuf1[C::TILE], vbuf1[C::TILE];
-  __shared__ int wred[2][RW];
-  const PrefixUnit u = prefix_unit(s, a);
+  __shared__ int wred[4][RW];
+  __shared__ float ml[KW == 2 ? RW * 128 : 1];
   const PrefixHdr p = *s.prefix;
+  const PrefixUnit u = prefix_unit(s, a);
   const int lab = a.layer_begin + u.li;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW;
   const int col = lane & 31, hh = lane >> 5;
 
-  const PrefixRow q = prefix_row(s, a, p, u.li, (u.rb * RW + rw) * 32 + col);
-  const PrefixSpan span = prefix_span(q);
-  if (lane == 0 && kw == 0) {
-    wred[0][rw] = span.lo;
-    wred[1][rw] = span.hi;
+  const int r0 = u.rb * RW * 32;
+  PrefixRow q = prefix_row(s, a, u.li, r0 + rw * 32 + col);
+  // half hh of the lane's query row (loaded before anything is known of the row; a row that sees
+  // nothing has no say)
+  f32x4 qv[D / 8];
+  {
+    const f32x4* qp = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.q) +
+                                                     (q.at * s.Hq + u.g * (s.Hq / s.Hkv) + q.head) * D + hh * (D / 2));
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) qv[k] = qp[k];
   }
-  __syncthreads();
-  int lo = INT_MAX, hi = 0;
-  for (int w = 0; w < RW; ++w) {
-    lo = min(lo, wred[0][w]);
-    hi = max(hi, wred[1][w]);
+  PrefixSpan span, all;  // (of the wave; of the WG)
+  const bool known = prefix_range(s, a, p, r0, RW * 32, &all);
+  if (!known) {  // a window: from the rows' positions
+    prefix_row_keys(s, a, p, q);
+    span = prefix_span(q);
+    all = prefix_range_of<RW>(span, rw, lane == 0 && kw == 0, wred);
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
+  const int lo = all.lo, hi = all.hi;
   // (splits hold whole 64-key tiles of pages, as in the bf16 pass; this WG's tiles are KEYS keys)
   const int first = hi > 0 ? lo / 64 : 0, tiles = hi > 0 ? (hi + 63) / 64 - first : 0;
   const int per = (tiles + a.splits - 1) / a.splits;
@@ -98,14 +104,17 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
   };
   auto pages_of = [&](int tile) __attribute__((always_inline)) { return tile_pages(p, (b0 + tile * C::KEYS) / 64); };
 
-  // half hh of the lane's query row
-  f32x4 qv[D / 8];
-  {
-    const bool some = q.lo < q.hi;
-    const f32x4* qp = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.q) +
-                                                     ((some ? q.at : 0) * s.Hq + u.g * (s.Hq / s.Hkv) + q.head) * D + hh * (D / 2));
-#pragma unroll
-    for (int k = 0; k < D / 8; ++k) qv[k] = some ? qp[k] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  // the first two tiles go out before anything that waits for the tries
+  TilePages next{};
+  if (n_tiles > 0) {
+    const TilePages pg0 = pages_of(0), pg1 = pages_of(min(1, n_tiles - 1));
+    issue(0, pg0, kbuf0, vbuf0);
+    if (n_tiles > 1) issue(1, pg1, kbuf1, vbuf1);
+    if (n_tiles > 2) next = pages_of(2);
+  }
+  if (known) {
+    prefix_row_keys(s, a, p, q);
+    span = prefix_span(q);
   }
   const float scale = a.scale_log2;
   float m = kPrefixNegBig, lsum = 0.0f;
@@ -115,12 +124,14 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[dt][v] = 0.0f;
 
-  TilePages next;
   auto step = [&](int tile, const unsigned char* kb, const unsigned char* vb, unsigned char* knext,
                   unsigned char* vnext) __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(kWaitVmAll);  // this thread's loads of the tile have landed
-    __syncthreads();                         // every thread's have; the other buffer is free
-    if (tile + 1 < n_tiles) {
+    // this thread's loads of the tile have landed, then every thread's, and the other buffer is free
+    // (the second tile is on its way already)
+    if (tile == 0 && n_tiles > 1) __builtin_amdgcn_s_waitcnt(wait_vm(2 * C::LOADS));
+    else __builtin_amdgcn_s_waitcnt(kWaitVmAll);
+    __syncthreads();
+    if (tile > 0 && tile + 1 < n_tiles) {
       issue(tile + 1, next, knext, vnext);
       if (tile + 2 < n_tiles) next = pages_of(tile + 2);
     }
@@ -150,7 +161,7 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int n = tb + 8 * (v >> 2) + 4 * hh + (v & 3);
-        acc[v] = (n >= q.lo) & (n < q.hi) & (n < b1) ? acc[v] : -INFINITY;
+        acc[v] = ((n >= q.lo) & (n < q.hi) & (n < b1)) ? acc[v] : -INFINITY;
       }
     }
     float tmax = acc[0];
@@ -222,10 +233,6 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
       for (int v = 0; v < 16; ++v) o[dt][v] += f[v];
     }
   };
-  if (n_tiles > 0) {
-    issue(0, pages_of(0), kbuf0, vbuf0);
-    if (n_tiles > 1) next = pages_of(1);
-  }
   for (int t = 0; t < n_tiles; t += 2) {
     step(t, kbuf0, vbuf0, kbuf1, vbuf1);
     if (t + 1 < n_tiles) step(t + 1, kbuf1, vbuf1, kbuf0, vbuf0);
@@ -237,7 +244,6 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
     __syncthreads();
     float* const o0 = reinterpret_cast<float*>(kbuf0);
     float* const o1 = reinterpret_cast<float*>(kbuf1);
-    float* const ml = reinterpret_cast<float*>(vbuf0);
     if (kw == 1) {
 #pragma unroll
       for (int x = 0; x < D / 4; ++x) {
@@ -264,31 +270,10 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
   }
 
   lsum += __shfl_xor(lsum, 32);
-  if (!q.in) return;
-  const bool some = q.lo < q.hi && lsum != 0.0f;
-  if (a.part != nullptr) {
-    float* rec = prefix_record(s, a, u, q);
-#pragma unroll
-    for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        float2* r2 = reinterpret_cast<float2*>(rec + 32 * dt + 8 * q4 + 4 * hh);
-        r2[0] = make_float2(o[dt][4 * q4], o[dt][4 * q4 + 1]);
-        r2[1] = make_float2(o[dt][4 * q4 + 2], o[dt][4 * q4 + 3]);
-      }
-    if (hh == 0) *reinterpret_cast<float2*>(rec + D) = make_float2(some ? m : kPrefixNegBig, some ? lsum : 0.0f);
-  } else {
-    float* orow = static_cast<float*>(a.out) + (q.at * s.Hq + u.g * (s.Hq / s.Hkv) + q.head) * D;
-#pragma unroll
-    for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        f32x4 y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = some ? o[dt][4 * q4 + e] / lsum : 0.0f;
-        *reinterpret_cast<f32x4*>(orow + 32 * dt + 8 * q4 + 4 * hh) = y;
-      }
-  }
+  if constexpr (KW == 1) __syncthreads();  // every wave has read its last tile
+  // (a K or V buffer of 32 keys holds a wave's rows; beside the second group's O, the V buffers do)
+  unsigned char* const mine = KW == 2 ? (rw == 0 ? vbuf0 : vbuf1) : rw == 0 ? kbuf0 : rw == 1 ? vbuf0 : rw == 2 ? kbuf1 : vbuf1;
+  prefix_output<float, D>(s, a, u, q, lane, m, lsum, o, reinterpret_cast<float*>(mine));
 }
 
 template <int D>

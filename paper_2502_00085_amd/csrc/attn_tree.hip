@@ -339,7 +339,7 @@ hipError_t launch_attn_tree(const DevState& s, const AttnArgs& a, long max_keys,
 #define LAUNCH_TREE_PFX(DD, PFX)                                                                      \
   (split ? hipExtLaunchKernelGGL((k_attn_tree<DD, 2, PFX>), grid, block, 0, st, ev0, ev1, 0, s, a)     \
          : hipExtLaunchKernelGGL((k_attn_tree<DD, 1, PFX>), grid, block, 0, st, ev0, ev1, 0, s, a))
-#define LAUNCH_TREE(DD) (a.prefix ? LAUNCH_TREE_PFX(DD, true) : LAUNCH_TREE_PFX(DD, false))
+#define LAUNCH_TREE(DD) (a.prefix_o ? LAUNCH_TREE_PFX(DD, true) : LAUNCH_TREE_PFX(DD, false))
   switch (s.D) {
     case 64: LAUNCH_TREE(64); break;
     case 96: LAUNCH_TREE(96); break;

@@ -138,10 +138,10 @@ __device__ inline void tree_output(const DevState& s, const AttnArgs& a, const T
   lsum += __shfl_xor(lsum, 32);
   if (q.r >= (PFX ? a.qn : a.qmax) * G) return;
   if (PFX && q.ok) {
-    const float* rec = a.prefix + ((((size_t)u.li * s.T + u.t) * a.qn + (q.owner - a.q0)) * s.Hq + u.g * G + q.r % G) *
-                                      a.prefix_splits * (D + 2);
-    for (int sp = 0; sp < a.prefix_splits; ++sp, rec += D + 2) {
-      const float m1 = rec[D], l1 = rec[D + 1];
+    const size_t rec0 = ((((size_t)u.li * s.T + u.t) * a.qn + (q.owner - a.q0)) * s.Hq + u.g * G + q.r % G) * a.prefix_splits;
+    for (int sp = 0; sp < a.prefix_splits; ++sp) {
+      const float* rec = a.prefix_o + (rec0 + sp) * D;
+      const float m1 = a.prefix_ml[rec0 + sp].x, l1 = a.prefix_ml[rec0 + sp].y;
       if (l1 == 0.0f) continue;  // (no key of the split)
       const float mn = fmaxf(m, m1);
       const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(m1 - mn);
@@ -151,13 +151,11 @@ __device__ inline void tree_output(const DevState& s, const AttnArgs& a, const T
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
-          // (records are D + 2 floats: 8-byte aligned)
-          const float2* r2 = reinterpret_cast<const float2*>(rec + 32 * dt + 8 * q4 + 4 * hh);
-          const float2 x = r2[0], y = r2[1];
+          const float4 x = *reinterpret_cast<const float4*>(rec + 32 * dt + 8 * q4 + 4 * hh);
           o[dt][4 * q4] = o[dt][4 * q4] * f0 + x.x * f1;
           o[dt][4 * q4 + 1] = o[dt][4 * q4 + 1] * f0 + x.y * f1;
-          o[dt][4 * q4 + 2] = o[dt][4 * q4 + 2] * f0 + y.x * f1;
-          o[dt][4 * q4 + 3] = o[dt][4 * q4 + 3] * f0 + y.y * f1;
+          o[dt][4 * q4 + 2] = o[dt][4 * q4 + 2] * f0 + x.z * f1;
+          o[dt][4 * q4 + 3] = o[dt][4 * q4 + 3] * f0 + x.w * f1;
         }
     }
   }

@@ -209,7 +209,7 @@ hipError_t launch_attn_tree_short(const DevState& s, const AttnArgs& a, hipStrea
                                   hipEvent_t ev1) {
   const dim3 grid(s.T * a.n_layers * s.Hkv * a.row_blocks), block(kTreeThreads);
 #define LAUNCH_SHORT(DD)                                                                                        \
-  (a.prefix ? hipExtLaunchKernelGGL((k_attn_tree_short<DD, true>), grid, block, 0, st, ev0, ev1, 0, s, a)       \
+  (a.prefix_o ? hipExtLaunchKernelGGL((k_attn_tree_short<DD, true>), grid, block, 0, st, ev0, ev1, 0, s, a)       \
             : hipExtLaunchKernelGGL((k_attn_tree_short<DD, false>), grid, block, 0, st, ev0, ev1, 0, s, a))
   switch (s.D) {
     case 64: LAUNCH_SHORT(64); break;

@@ -145,9 +145,9 @@ td::DevState prefix_state(const td_ctx* c) {
 // Layers of one launch beside a prefix pass: `rows` query rows (owners of them per trie) of a KV head.
 int prefix_layers(const td_ctx* c, int n_layers, int owners, int rows) {
   const td::DevState& s = c->dev;
-  const size_t rec = s.D + 2, padded = (size_t)(rows + 31) / 32 * 32;
-  const size_t fit = std::min(c->prefix_floats / ((size_t)s.T * owners * s.Hq * rec),
-                              c->prefix_trie_floats / ((size_t)s.T * s.Hkv * padded * rec));
+  const size_t padded = (size_t)(rows + 31) / 32 * 32;
+  const size_t fit = std::min(c->prefix_records / ((size_t)s.T * owners * s.Hq),
+                              c->prefix_trie_floats / ((size_t)s.T * s.Hkv * padded * (s.D + 2)));
   return (int)std::max<size_t>(1, std::min<size_t>(n_layers, fit));
 }
 
@@ -444,9 +444,9 @@ td_status trie_tree_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32
     // the key range streamed once for all of them).  With a shared prefix: as many layers, and
     // where one layer's records exceed the workspace as many queries, per launch as it holds.
     const int tpb = td::attn_tree_rows_per_block();
-    const size_t query = (size_t)s.T * s.Hq * (s.D + 2);  // floats of the records of one query per trie
-    const int lc = !prefix ? n_layers : (int)std::max<size_t>(1, std::min<size_t>(n_layers, c->prefix_floats / (query * q_max)));
-    const int qc = !prefix || lc > 1 ? q_max : (int)std::max<size_t>(1, std::min<size_t>(q_max, c->prefix_floats / query));
+    const size_t query = (size_t)s.T * s.Hq;  // records of one query per trie
+    const int lc = !prefix ? n_layers : (int)std::max<size_t>(1, std::min<size_t>(n_layers, c->prefix_records / (query * q_max)));
+    const int qc = !prefix || lc > 1 ? q_max : (int)std::max<size_t>(1, std::min<size_t>(q_max, c->prefix_records / query));
     const long nodes = max_nodes(c, false);
     // (nearly every node a query, and no window that cuts their ranges)
     const bool ramp = qc >= nodes - nodes / 8 && (s.W <= 0 || s.W >= nodes);
@@ -463,7 +463,8 @@ td_status trie_tree_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32
           // (few splits: every row merges their records by itself, one after the other)
           e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, q0, a.qn, q_max, d_qslots, a.q, a.scale_log2, 8, st, first,
                               &a.prefix_splits);
-          a.prefix = c->prefix_part;
+          a.prefix_o = c->prefix_o;
+          a.prefix_ml = c->prefix_ml;
           first = nullptr;
         }
         if (e == hipSuccess)
@@ -490,7 +491,7 @@ td_status trie_tree_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32
     a.half_wgs = a.splits > 1 && c->splits_override == 0 && sp.half_wgs;
     a.xcd_group = a.row_blocks > 1 && ((long)s.T * a.n_layers * s.Hkv * a.splits) % 8 == 0 ? 1 : 0;
     a.partial = a.splits > 1 || prefix;
-    int prefix_splits = 0;
+      int prefix_splits = 0;
     if (prefix)
       e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, 0, q_max, q_max, d_qslots, a.q, a.scale_log2, 64, st, first,
                           &prefix_splits);

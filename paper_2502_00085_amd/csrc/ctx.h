@@ -26,9 +26,10 @@ struct td_ctx {
   int32_t prefix_length = 0, prefix_room = 0;
   int32_t* prefix_table = nullptr;     // device, room for prefix_table_cap entries and the padding
   size_t prefix_table_cap = 0;
-  float* prefix_part = nullptr;        // records of a pass, and the tries' partials beside it
+  float* prefix_o = nullptr;           // records of a pass (PrefixArgs), and the tries' partials beside it
+  float2* prefix_ml = nullptr;
   float* prefix_trie_part = nullptr;
-  size_t prefix_floats = 0, prefix_trie_floats = 0;
+  size_t prefix_records = 0, prefix_trie_floats = 0;
   hipEvent_t ev[4][2] = {};             // td_set_kernel_events: per td_phase, the
                                        //   kernel-timestamp events of its next run
   std::vector<void*> allocs;
@@ -51,7 +52,7 @@ hipError_t copy_due_rows(td_ctx* c, int layer_begin, int n_layers, hipStream_t s
 
 // The pass over the shared prefix for the tries' rows (prefix.cpp): leaves (q_max = b, no qslots) or
 // stored nodes (queries q0 .. q0 + qn - 1 of each trie), at most max_splits splits.  Returns the splits
-// of its records in prefix_part.
+// of its records.
 hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int q0, int qn, int q_max,
                        const int32_t* d_qslots, const void* d_q, float scale_log2, int max_splits, hipStream_t st,
                        hipEvent_t ev0, int* splits);

@@ -71,7 +71,8 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   const DevState& s = c->dev;
   PrefixArgs a{};
   a.q = d_q;
-  a.part = c->prefix_part;
+  a.part_o = c->prefix_o;
+  a.part_ml = c->prefix_ml;
   a.qslots = d_qslots;
   a.rows = nodes ? PrefixRows::kNodes : PrefixRows::kLeaves;
   a.layer_begin = layer_begin;
@@ -85,8 +86,8 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   const int rpb = prefix_rows_per_block(s, rows);
   a.row_blocks = (int)((rows + rpb - 1) / rpb);
   const long keys = s.W > 0 ? std::min(c->prefix_length, s.W) : c->prefix_length;
-  const long fit = (long)(c->prefix_floats / ((size_t)n_layers * s.T * qn * s.Hq * (s.D + 2)));
-  a.splits = prefix_splits(s, rows, (long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
+  const long fit = (long)(c->prefix_records / ((size_t)n_layers * s.T * qn * s.Hq));
+  a.splits = prefix_splits((long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
   a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
   *splits = a.splits;
   return launch_prefix(s, a, st, ev0, nullptr);
@@ -95,7 +96,8 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
 hipError_t prefix_merge(td_ctx* c, bool nodes, const AttnArgs& a, int splits, int block_rows, int q_max, hipStream_t st,
                         hipEvent_t ev1) {
   PrefixMergeArgs m{};
-  m.prefix = c->prefix_part;
+  m.prefix_o = c->prefix_o;
+  m.prefix_ml = c->prefix_ml;
   m.prefix_splits = splits;
   m.trie = c->prefix_trie_part;
   m.trie_splits = a.splits;
@@ -151,15 +153,15 @@ td_status td_set_prefix(td_ctx* c, const td_prefix* d) {
       e = reserve(c, &c->prefix_table, 2 * table.size());
       if (e == hipSuccess) c->prefix_table_cap = 2 * table.size();
     }
-    if (e == hipSuccess && c->prefix_floats == 0) {
-      const size_t rec = s.D + 2, G = s.Hq / s.Hkv;
-      const size_t rows = std::max<size_t>(s.b * G, 128), heads = (size_t)s.T * s.Hkv;
-      const size_t floats = std::max(kWorkFloats, heads * rows * rec);
-      const size_t trie_floats = std::max(kWorkFloats, heads * ((rows + 31) / 32 * 32) * rec);
-      e = reserve(c, &c->prefix_part, floats);
+    if (e == hipSuccess && c->prefix_records == 0) {
+      const size_t G = s.Hq / s.Hkv, rows = std::max<size_t>(s.b * G, 128), heads = (size_t)s.T * s.Hkv;
+      const size_t records = std::max(kWorkFloats / s.D, heads * rows);
+      const size_t trie_floats = std::max(kWorkFloats, heads * ((rows + 31) / 32 * 32) * (s.D + 2));
+      e = reserve(c, &c->prefix_o, records * s.D);
+      if (e == hipSuccess) e = reserve(c, &c->prefix_ml, records);
       if (e == hipSuccess) e = reserve(c, &c->prefix_trie_part, trie_floats);
       if (e == hipSuccess) {
-        c->prefix_floats = floats;
+        c->prefix_records = records;
         c->prefix_trie_floats = trie_floats;
       }
     }
@@ -251,16 +253,18 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
   const int rpb = td::prefix_rows_per_block(s, rows);
   a.row_blocks = (int)((rows + rpb - 1) / rpb);
   const long keys = s.W > 0 ? std::min(pos + n, s.W) : pos + n;
-  const long fit = (long)(c->prefix_floats / ((size_t)n_layers * n * s.Hq * (s.D + 2)));
-  a.splits = td::prefix_splits(s, rows, (long)n_layers * s.Hkv * a.row_blocks, keys, std::max(1l, fit));
+  const long fit = (long)(c->prefix_records / ((size_t)n_layers * n * s.Hq));
+  a.splits = td::prefix_splits((long)n_layers * s.Hkv * a.row_blocks, keys, std::max(1l, fit));
   a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
-  a.part = a.splits > 1 ? c->prefix_part : nullptr;
+  a.part_o = a.splits > 1 ? c->prefix_o : nullptr;
+  a.part_ml = c->prefix_ml;
   hipEvent_t ev0 = c->ev[TD_PHASE_ATTN][0], ev1 = c->ev[TD_PHASE_ATTN][1];
   c->ev[TD_PHASE_ATTN][0] = c->ev[TD_PHASE_ATTN][1] = nullptr;
-  hipError_t e = td::launch_prefix(s, a, st, ev0, a.part ? nullptr : ev1);
-  if (e == hipSuccess && a.part) {
+  hipError_t e = td::launch_prefix(s, a, st, ev0, a.part_o ? nullptr : ev1);
+  if (e == hipSuccess && a.part_o) {
     td::PrefixMergeArgs m{};
-    m.prefix = c->prefix_part;
+    m.prefix_o = c->prefix_o;
+  m.prefix_ml = c->prefix_ml;
     m.prefix_splits = a.splits;
     m.out = d_out;
     m.rows = td::PrefixRows::kChunk;

@@ -11,11 +11,13 @@ enum class PrefixRows { kLeaves, kNodes, kChunk };
 
 // One pass over the prefix.  Row owner o in [0, tries * per_trie) is query q0 + o % per_trie of trie
 // o / per_trie (kChunk: one "trie", whose query j sits at position pos0 + j); a row is a (owner,
-// query head of one KV head) pair.  Each (row, split) leaves a record of D + 2 floats - O, the shift
-// m (log2 domain) and the sum l - at part[((li * owners + o) * Hq + head) * splits + split].
+// query head of one KV head) pair.  Each (row, split) leaves a record, number ((li * owners + o) * Hq +
+// head) * splits + split: D floats O at part_o, the shift m (log2 domain) and the sum l at part_ml.  A
+// record with l = 0 (no key of the split) has no O.
 struct PrefixArgs {
   const void* q;                    // [n_layers][tries][q_stride][Hq][D]
-  float* part;                      // records, or null: out gets O / l (splits == 1)
+  float* part_o;                    // records, or null: out gets O / l (splits == 1)
+  float2* part_ml;
   void* out;                        // as q
   const int32_t* qslots = nullptr;  // (kNodes) [tries][q_stride]
   PrefixRows rows;
@@ -29,9 +31,8 @@ struct PrefixArgs {
 
 // Query rows of a workgroup for a pass of this many rows per KV head.
 int prefix_rows_per_block(const DevState& s, long rows);
-// Splits of the prefix's keys for `units` (layer, KV head, row block) units over `keys` keys, at most
-// `most`.
-int prefix_splits(const DevState& s, long rows, long units, long keys, long most);
+// Splits of `keys` keys for `units` (layer, KV head, row block) units, at most `most`.
+int prefix_splits(long units, long keys, long most);
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
                            hipEvent_t ev1);
@@ -39,7 +40,8 @@ hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_
 // Merges a pass's records with those of the tries (attention partials of `splits` splits in blocks of
 // block_rows rows, null: none) into out.
 struct PrefixMergeArgs {
-  const float* prefix;
+  const float* prefix_o;
+  const float2* prefix_ml;
   int prefix_splits;
   const float* trie;
   int trie_splits, block_rows, row_blocks;
