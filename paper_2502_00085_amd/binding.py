@@ -142,9 +142,10 @@ def _check(ctx, st: int):
 
 
 def _stream(stream) -> Optional[int]:
-    import torch
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # (the handle alone: building a torch.cuda.Stream around it costs a call 2 us of host time)
+        import torch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -250,34 +251,36 @@ def td_set_prefix(ctx, dims: Dims, k_pages, v_pages=None, pages: Sequence[int] =
     _check(ctx, lib().td_set_prefix(ctx, ctypes.byref(d)))
 
 
-def _rows(t, dtype, lead, heads, dim, name):
-    """Address and row stride of t [lead..][heads][dim]: a device tensor whose rows are contiguous and
-    follow one another at one distance (a slice of a fused projection)."""
+def _rows(t, dtype, shape, name):
+    """Address and row stride of t [..][heads][dim]: a device tensor whose rows are contiguous and follow
+    one another at one distance (a slice of a fused projection)."""
     if t is None:
         return None, 0
-    shape = tuple(lead) + (heads, dim)
-    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape:
+    if not t.is_cuda or t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be a device tensor of {dtype} and shape {list(shape)}, got {t.dtype}, {list(t.shape)}")
-    rows = [(n, st) for n, st in zip(t.shape[:-2], t.stride()[:-2]) if n != 1]
+    heads, dim = shape[-2:]
+    if t.is_contiguous():
+        return t.data_ptr(), heads * dim
+    strides = t.stride()
+    rows = [(n, st) for n, st in zip(shape[:-2], strides[:-2]) if n != 1]
     row = rows[-1][1] if rows else heads * dim
-    ok = (dim == 1 or t.stride(-1) == 1) and (heads == 1 or t.stride(-2) == dim)
+    ok = strides[-1] == 1 and (heads == 1 or strides[-2] == dim)
     for n, st in reversed(rows):
         ok = ok and st == row
         row *= n
     if not ok:
-        raise ValueError(f"{name}: rows must be contiguous and equally far apart, got strides {t.stride()}")
+        raise ValueError(f"{name}: rows must be contiguous and equally far apart, got strides {strides}")
     return t.data_ptr(), rows[-1][1] if rows else heads * dim
 
 
 def _store_rows(dims: Dims, lead, k, v, q, q_out):
     import torch
     tdt = torch.float32 if dims.dtype == TD_F32 else torch.bfloat16
-    (qp, qs), (kp, ks), (vp, vs) = (_rows(q, tdt, lead, dims.Hq, dims.D, "q"), _rows(k, tdt, lead, dims.Hkv, dims.D, "k"),
-                                    _rows(v, tdt, lead, dims.Hkv, dims.D, "v"))
-    n = dims.Hq * dims.D
-    for x in lead:
-        n *= x
-    return qp, qs, kp, ks, vp, vs, _ptr(q_out, tdt, n, "q_out")
+    q_shape, kv_shape = torch.Size((*lead, dims.Hq, dims.D)), torch.Size((*lead, dims.Hkv, dims.D))
+    qp, qs = _rows(q, tdt, q_shape, "q")
+    kp, ks = _rows(k, tdt, kv_shape, "k")
+    vp, vs = _rows(v, tdt, kv_shape, "v")
+    return qp, qs, kp, ks, vp, vs, _ptr(q_out, tdt, q_shape.numel(), "q_out")
 
 
 def trie_prefix_store(ctx, dims: Dims, layer_begin: int, n_layers: int, pos: int, k, v, q=None, q_out=None,

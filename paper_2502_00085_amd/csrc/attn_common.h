@@ -132,6 +132,38 @@ __device__ inline void move_rows_regs(const DevState& s, int t, int l, int g) {
   __syncthreads();
 }
 
+// Merges the shared prefix's records of an output row (a.prefix_o, in the order of the rows of out)
+// into its state: elements c .. c + E - 1 of O, the shift M (log2 domain) and the sum L.  A record with
+// sum 0 weighs nothing; a NaN sum makes the row NaN.
+template <int E>
+__device__ inline void merge_prefix(const DevState& s, const AttnArgs& a, size_t row, int c, float& M, float& L, float (&O)[E]) {
+  for (int sp = 0; sp < a.prefix_splits; ++sp) {
+    const size_t r = row * a.prefix_splits + sp;
+    const float2 ml = a.prefix_ml[r];
+    const float* o = a.prefix_o + r * s.D + c;
+    float x[E];
+    if constexpr (E % 4 == 0) {
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(o + e);
+        x[e] = v.x;
+        x[e + 1] = v.y;
+        x[e + 2] = v.z;
+        x[e + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = o[e];
+    }
+    if (ml.y == 0.0f) continue;
+    const float Mn = fmaxf(M, ml.x), f0 = __builtin_amdgcn_exp2f(M - Mn), f1 = __builtin_amdgcn_exp2f(ml.x - Mn);
+    M = Mn;
+    L = L * f0 + ml.y * f1;
+#pragma unroll
+    for (int e = 0; e < E; ++e) O[e] = O[e] * f0 + x[e] * f1;
+  }
+}
+
 // Stores the pending leaves' K/V rows of one (trie, layer, KV head) into the pools
 // (16-byte chunks, whole block).
 template <typename T>

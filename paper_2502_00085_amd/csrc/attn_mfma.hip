@@ -677,17 +677,22 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_mfma(DevState s, AttnArgs a
         O[0] += x0.x * f; O[1] += x0.y * f; O[2] += x0.z * f; O[3] += x0.w * f;
         O[4] += x1.x * f; O[5] += x1.y * f; O[6] += x1.z * f; O[7] += x1.w * f;
       }
-      const float Mi = rowm[i], L = rowl[i];
+      float Mi = rowm[i], L = rowl[i];
       if (!a.partial) {
         const int rr = (u.rb * RB + rbk) * kRows + i;
         if (rr < nrows * G) {
           const int bm = rr / G;
-          const bool live = (TREE || bm < n_live) && L > 0.0f;
+          const size_t row = (((size_t)u.li * s.T + u.t) * nrows + bm) * s.Hq + u.g * G + rr % G;
+          bool live = (TREE || bm < n_live) && L > 0.0f;
+          if (a.prefix_o != nullptr) {
+            merge_prefix(s, a, row, c, Mi, L, O);
+            live = (TREE || bm < n_live) && L != 0.0f;  // (a NaN sum: a NaN row)
+          }
           const float inv = live ? 1.0f / L : 0.0f;
           bf16x8 y;
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] = (__bf16)(O[e] * inv);
-          *reinterpret_cast<bf16x8*>(outp + ((((size_t)u.li * s.T + u.t) * nrows + bm) * s.Hq + u.g * G + rr % G) * D + c) = y;
+          *reinterpret_cast<bf16x8*>(outp + row * D + c) = y;
         }
       } else {
         float* pp = part + ((size_t)u.split * kRows + i) * (D + 2);

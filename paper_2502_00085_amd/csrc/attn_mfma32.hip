@@ -412,13 +412,20 @@ __global__ __launch_bounds__((Cfg32<T, D, RT>::NW * 64), (Cfg32<T, D, RT>::NW / 
       const float f = fw[w * C::ROWS + i];
       O += *reinterpret_cast<const f32x4*>(obuf + (w * C::ROWS + i) * C::OS + c) * f;
     }
-    const float L = rowl[i];
+    float L = rowl[i];
     if (!a.partial) {
       const int r = u.rb * C::ROWS + i;
       if (r < s.b * G) {
         const int bm = r / G;
-        const bool live = bm < n_live && L > 0.0f;
-        T* dst = outp + ((((size_t)u.li * s.T + u.t) * s.b + bm) * s.Hq + u.g * G + r % G) * D + c;
+        const size_t row = (((size_t)u.li * s.T + u.t) * s.b + bm) * s.Hq + u.g * G + r % G;
+        bool live = bm < n_live && L > 0.0f;
+        if (a.prefix_o != nullptr) {
+          float M = rowm[i], o4[4] = {O[0], O[1], O[2], O[3]};
+          merge_prefix(s, a, row, c, M, L, o4);
+          O = f32x4{o4[0], o4[1], o4[2], o4[3]};
+          live = bm < n_live && L != 0.0f;  // (a NaN sum: a NaN row)
+        }
+        T* dst = outp + row * D + c;
         typedef T t4 __attribute__((ext_vector_type(4)));
         t4 y;
 #pragma unroll

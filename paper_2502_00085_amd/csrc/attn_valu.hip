@@ -180,8 +180,16 @@ __global__ __launch_bounds__(kValuThreads) void k_attn_valu(DevState s, AttnArgs
       const int r = u.rb * R + i;
       if (r < s.b * G) {
         const int bm = r / G, hl = r % G;
-        const float val = (bm < n_live && L > 0.0f) ? O / L : 0.0f;
-        outp[((((size_t)u.li * s.T + u.t) * s.b + bm) * s.Hq + u.g * G + hl) * DD + c] = from_f<T>(val);
+        const size_t row = (((size_t)u.li * s.T + u.t) * s.b + bm) * s.Hq + u.g * G + hl;
+        bool live = bm < n_live && L > 0.0f;
+        if (a.prefix_o != nullptr) {
+          float o1[1] = {O};
+          merge_prefix(s, a, row, c, M, L, o1);
+          O = o1[0];
+          live = bm < n_live && L != 0.0f;  // (a NaN sum: a NaN row)
+        }
+        const float val = live ? O / L : 0.0f;
+        outp[row * DD + c] = from_f<T>(val);
       }
     } else {
       float* pp = part + ((size_t)u.split * R + i) * (DD + 2);

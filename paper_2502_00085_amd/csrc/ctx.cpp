@@ -205,9 +205,10 @@ hipError_t attn_layers(td_ctx* c, int layer_begin, int n_layers, const void* d_q
   int prefix_splits = 0;
   if (e == hipSuccess && prefix)
     e = td::prefix_pass(c, false, layer_begin, n_layers, 0, s.b, s.b, nullptr, d_q, scale_log2, 64, st, ev0, &prefix_splits);
-  a.partial = a.splits > 1 || prefix;
+  const bool fold = prefix && td::prefix_fold(c, a, prefix_splits);
+  a.partial = a.splits > 1 || (prefix && !fold);
   if (e == hipSuccess) e = td::launch_attn(kernel, s, a, st, prefix ? nullptr : ev0, a.partial ? nullptr : ev1);
-  if (e == hipSuccess && prefix) {
+  if (e == hipSuccess && prefix && !fold) {
     e = td::prefix_merge(c, false, a, prefix_splits, rpb, s.b, st, ev1);
   } else if (e == hipSuccess && a.splits > 1) {
     td::AttnArgs ac = a;  // the combine runs per 32-row block
@@ -495,8 +496,10 @@ td_status trie_tree_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32
     if (prefix)
       e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, 0, q_max, q_max, d_qslots, a.q, a.scale_log2, 64, st, first,
                           &prefix_splits);
+    const bool fold = prefix && td::prefix_fold(c, a, prefix_splits);
+    a.partial = a.splits > 1 || (prefix && !fold);
     if (e == hipSuccess) e = td::launch_attn_mfma(ds, a, st, prefix ? nullptr : first, a.partial ? nullptr : last);
-    if (e == hipSuccess && prefix) e = td::prefix_merge(c, true, a, prefix_splits, rpb, q_max, st, last);
+    if (e == hipSuccess && prefix && !fold) e = td::prefix_merge(c, true, a, prefix_splits, rpb, q_max, st, last);
     else if (e == hipSuccess && a.splits > 1) e = td::launch_attn_combine(ds, a, rpb, st, nullptr, last);
   }
   if (e != hipSuccess) return hip_fail(c, e, "trie_tree_attn launch");

@@ -56,7 +56,10 @@ hipError_t copy_due_rows(td_ctx* c, int layer_begin, int n_layers, hipStream_t s
 hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int q0, int qn, int q_max,
                        const int32_t* d_qslots, const void* d_q, float scale_log2, int max_splits, hipStream_t st,
                        hipEvent_t ev0, int* splits);
-// Merges them with the tries' partials (a: of the attention launch, block_rows rows per block).
+// Whether an unsplit attention launch merges that many splits of records into its output itself (a:
+// gets the records), which saves its partials and a launch.
+bool prefix_fold(const td_ctx* c, AttnArgs& a, int splits);
+// Else merges them with the tries' partials (a: of the attention launch, block_rows rows per block).
 hipError_t prefix_merge(td_ctx* c, bool nodes, const AttnArgs& a, int splits, int block_rows, int q_max, hipStream_t st,
                         hipEvent_t ev1);
 

@@ -13,6 +13,9 @@ using td::hip_fail;
 
 namespace {
 
+// Records an attention launch merges by itself, one after the other: more are merged by a launch of
+// their own, eight at a time.
+constexpr int kFoldSplits = 4;
 constexpr size_t kWorkFloats = 16u << 20;  // of either workspace, unless one layer needs more
 
 td_status bad_layers(td_ctx* c, int layer_begin, int n_layers) {
@@ -91,6 +94,15 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
   *splits = a.splits;
   return launch_prefix(s, a, st, ev0, nullptr);
+}
+
+bool prefix_fold(const td_ctx* c, AttnArgs& a, int splits) {
+  a.prefix_o = nullptr;
+  if (a.splits > 1 || splits > kFoldSplits) return false;
+  a.prefix_o = c->prefix_o;
+  a.prefix_ml = c->prefix_ml;
+  a.prefix_splits = splits;
+  return true;
 }
 
 hipError_t prefix_merge(td_ctx* c, bool nodes, const AttnArgs& a, int splits, int block_rows, int q_max, hipStream_t st,

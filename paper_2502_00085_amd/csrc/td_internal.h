@@ -127,10 +127,12 @@ struct AttnArgs {
                                    // grid's row_blocks counts WGs, of rb_per_wg blocks each
   int all_splits = 0;              // (matrix-core kernel) 1: every split WG takes a share of the
                                    // nodes (a forced split count); 0: only as many as needed
-  int partial = 0;                 // 1: the split partials, also of one split (a merge follows)
-  const float* prefix_o = nullptr; // (prefill-shaped tree kernels) records of the shared prefix to merge
-  const float2* prefix_ml = nullptr;  // (PrefixArgs::part_o, part_ml), of queries q0 .. q0 + qn - 1 of each
-  int prefix_splits = 0;           //   trie, which are the launch's queries; null: every query, no prefix
+  int partial = 0;                 // 1: partials, of one split too (a merge follows); 0: the output
+  // records of the shared prefix (PrefixArgs::part_o, part_ml) to merge into the output; null: none
+  const float* prefix_o = nullptr;
+  const float2* prefix_ml = nullptr;
+  int prefix_splits = 0;
+  // (prefill-shaped tree kernels beside a prefix) the launch's queries, q0 .. q0 + qn - 1 of each trie
   int q0 = 0, qn = 0;
   int half_wgs = 0;                // (matrix-core kernel) 1: 4-wave WGs, two per CU (two row blocks:
                                    // no fused row copy, moves == 0)

@@ -244,16 +244,26 @@ def test_row_strides_of_a_fused_projection():
         def stride(self, *a):
             return self.t.stride(*a)
 
+        def is_contiguous(self):
+            return self.t.is_contiguous()
+
         def data_ptr(self):
             return 4096
 
     bf = torch.bfloat16
     fused = torch.zeros((2, 3, 5, 40 * 8 + 16), dtype=bf)
     part = fused[..., 8:8 + 32].unflatten(-1, (4, 8))
-    assert B._rows(Dev(part), bf, (2, 3, 5), 4, 8, "x") == (4096, 336)
-    assert B._rows(Dev(part[:1, :1, :1]), bf, (1, 1, 1), 4, 8, "x") == (4096, 32)
-    assert B._rows(Dev(part[:1]), bf, (1, 3, 5), 4, 8, "x") == (4096, 336)
-    assert B._rows(None, bf, (1,), 4, 8, "x") == (None, 0)
+    def rows(t):
+        return B._rows(Dev(t), bf, t.shape, "x")
+
+    assert rows(part) == (4096, 336)
+    assert rows(part[:1, :1, :1]) == (4096, 32)
+    assert rows(part[:1]) == (4096, 336)
+    assert rows(part.contiguous()) == (4096, 32)
+    assert rows(part[:, :, :, :1]) == (4096, 336)
+    assert B._rows(None, bf, (1,), "x") == (None, 0)
     for bad in (part[:, :, :4], part.transpose(1, 2), part[..., :4], part[..., ::2, :]):
         with pytest.raises(ValueError):
-            B._rows(Dev(bad), bf, tuple(bad.shape[:-2]), *bad.shape[-2:], "x")
+            rows(bad)
+    with pytest.raises(ValueError):
+        B._rows(Dev(part), bf, torch.Size((2, 3, 5, 8, 4)), "x")
