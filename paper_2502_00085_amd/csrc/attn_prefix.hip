@@ -23,7 +23,7 @@ namespace {
 constexpr float kMost = 8192.0f;  // a row's shift moves once 16 of its probabilities add up to more
 constexpr float kSlack = 8.0f;    // ... to its largest score, if that is 2^8 above
 
-// RW waves hold 32 rows each; KW groups of RW waves take the 32-key halves of each tile in turn.
+// RW waves hold 32 rows each; KW groups of RW waves take the 32-key halves of each tile.
 template <int D, int RW, int KW>
 struct PrefixCfg {
   static constexpr int THREADS = 64 * RW * KW;
@@ -32,23 +32,22 @@ struct PrefixCfg {
   static constexpr int CPR = D / 8;        // 16-byte chunks per key row
   static constexpr int NBLK = CPR / 4;     // 64-byte blocks per row
   static constexpr int HALF = 32 * D * 2;  // bytes of 32 K (or V) rows
-  static constexpr int CHUNKS = 2 * HALF / 16;           // of K (or V) of a tile
-  static constexpr int LOADS = (CHUNKS + THREADS - 1) / THREADS;  // 16-byte loads per thread
-  static constexpr bool RAGGED = CHUNKS % THREADS != 0;  // (the last of them by some of the waves)
-  static_assert(CHUNKS % 64 == 0, "a tile is a whole number of wave loads");
+  static constexpr int LOADS = 2 * HALF / 16 / THREADS;  // 16-byte loads per thread: K (or V) of a tile
+  static_assert(2 * HALF % (16 * THREADS) == 0, "a tile is a whole number of WG loads");
   static constexpr bool ONE_OFS = THREADS % CPR == 0 && (THREADS / CPR) % CPR == 0;
   static constexpr int OFS = ONE_OFS ? 1 : LOADS;
-  static constexpr int WAVES = D <= 128 || THREADS == 512 ? 2 : 1;  // per SIMD, as the LDS allows
+  static constexpr int WAVES = 8 * HALF <= 80 * 1024 ? 2 : 1;  // per SIMD, as the LDS allows
   static constexpr int VROT = 8 % NBLK == 0 ? 1 : 4;  // rotations of V rows 8 apart
 };
 
 template <int D, int RW, int KW>
 __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k_attn_prefix(DevState s, PrefixArgs a) {
   using C = PrefixCfg<D, RW, KW>;
+  static_assert(2 * C::LOADS < 64, "the wait counter holds a tile's loads");
   static_assert(KW == 1 || KW == 2, "one or two groups");
   constexpr int NH = 2 / KW;  // 32-key halves of a tile per wave
-  // (four arrays, each used for one buffer only: the compiler can tell an operand read of one buffer
-  // from the direct loads under way into the other)
+  // (an array per buffer: the compiler can tell an operand read of one buffer from the direct loads
+  // under way into the others)
   __shared__ __attribute__((aligned(16))) unsigned char kbuf0[2 * C::HALF], vbuf0[2 * C::HALF];
   __shared__ __attribute__((aligned(16))) unsigned char kbuf1[2 * C::HALF], vbuf1[2 * C::HALF];
   __shared__ int wred[4][RW];
@@ -113,7 +112,6 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     const int last = hi - 1 - tb;  // (rows past the end: the last row)
 #pragma unroll
     for (int j = 0; j < C::LOADS; ++j) {
-      if (C::RAGGED && j * C::THREADS + wave * 64 >= C::CHUNKS) break;
       const uint32_t step = C::ONE_OFS ? j * (C::THREADS / C::CPR) * 2 * D : 0;
       uint32_t ko = kofs[C::ONE_OFS ? 0 : j], vo = vofs[C::ONE_OFS ? 0 : j];
       const unsigned char *ks = kt + step, *vs = vt + step;
@@ -142,7 +140,12 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     }
   };
 
-  // the first two tiles go out before anything that waits for the tries
+  // (what waits for the tries comes first: loads return in order, and these must not wait for tiles)
+  if (known) {
+    prefix_row_keys(s, a, p, q);
+    span = prefix_span(q);
+  }
+  // the first two tiles
   TilePages next{};
   if (t0 < t1) {
     const bool main = m0 < m1;
@@ -152,10 +155,6 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     issue(x0, pg0, kbuf0, vbuf0);
     if (two) issue(x1, pg1, kbuf1, vbuf1);
     if (m0 + 2 < m1) next = tile_pages(p, m0 + 2);
-  }
-  if (known) {
-    prefix_row_keys(s, a, p, q);
-    span = prefix_span(q);
   }
   const int grp = lane >> 4, tm = (lane & 15) >> 2, tq = lane & 3;
   int kread[C::KSTEPS], vread[C::VROT][C::DT];
@@ -232,7 +231,7 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
                   unsigned char* vnext) __attribute__((always_inline)) {
     // this thread's loads of the tile have landed, then every thread's, and the other buffer is free
     // (the second tile is on its way already)
-    if (!C::RAGGED && tile == m0 && m0 + 1 < m1) __builtin_amdgcn_s_waitcnt(wait_vm(2 * C::LOADS));
+    if (tile == m0 && m0 + 1 < m1) __builtin_amdgcn_s_waitcnt(wait_vm(2 * C::LOADS));
     else __builtin_amdgcn_s_waitcnt(kWaitVmAll);
     __syncthreads();
     if (tile > m0 && tile + 1 < m1) {
@@ -372,9 +371,12 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
 template <int D>
 void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
   const dim3 grid(a.n_layers * s.Hkv * a.splits * a.row_blocks);
-  if (rpb == 32) hipExtLaunchKernelGGL((k_attn_prefix<D, 1, 2>), grid, dim3(128), 0, st, ev0, ev1, 0, s, a);
-  else if (rpb == 64) hipExtLaunchKernelGGL((k_attn_prefix<D, 2, 2>), grid, dim3(256), 0, st, ev0, ev1, 0, s, a);
-  else hipExtLaunchKernelGGL((k_attn_prefix<D, 4, 1>), grid, dim3(256), 0, st, ev0, ev1, 0, s, a);
+#define LAUNCH_PREFIX(RW, KW) \
+  hipExtLaunchKernelGGL((k_attn_prefix<D, RW, KW>), grid, dim3(64 * RW * KW), 0, st, ev0, ev1, 0, s, a)
+  if (rpb == 32) LAUNCH_PREFIX(1, 2);
+  else if (rpb == 64) LAUNCH_PREFIX(2, 2);
+  else LAUNCH_PREFIX(4, 1);
+#undef LAUNCH_PREFIX
 }
 
 // Each (row, 8-element chunk of d) is merged by TP adjacent lanes, lane j taking the groups of 8
@@ -478,10 +480,11 @@ int prefix_rows_per_block(const DevState& s, long rows) {
 // shorter chains of tiles and more records to merge.  Measured, 8 KV heads at d = 128, the pass and
 // its merge, us: 128 rows over 4,096 keys, 8 / 16 / 32 splits: 22.6 / 20.9 / 24.6; over 16,384 keys, 16 /
 // 32 / 64: 35.1 / 30.5 / 34.1; 1,024 rows (8 blocks) over 1,024 keys, 4 / 8: 25.5 / 27.7; over 8,192 keys,
-// 4 / 8 / 16: 63 / 57 / 72; 32 rows over 4,096 keys, 16 / 32 / 64: 17.4 / 17.9 / 20.1.
-int prefix_splits(long units, long keys, long most) {
-  const long tiles = (keys + 63) / 64;
-  const long one = std::min((256 + units - 1) / units, tiles / 4), two = std::min((512 + units - 1) / units, tiles / 16);
+// 4 / 8 / 16: 63 / 57 / 72; 32 rows over 4,096 keys, 16 / 32 / 64: 17.4 / 17.9 / 20.1.  In fp32 a tile takes
+// ten times as long: one tile, and two per CU where each still has 2.
+int prefix_splits(const DevState& s, long units, long keys, long most) {
+  const long tiles = (keys + 63) / 64, few = s.dtype == TD_F32 ? 1 : 4, many = s.dtype == TD_F32 ? 2 : 16;
+  const long one = std::min((256 + units - 1) / units, tiles / few), two = std::min((512 + units - 1) / units, tiles / many);
   return (int)std::max(1l, std::min(std::max(one, two), most));
 }
 

@@ -1,14 +1,20 @@
 // Attention over the shared prefix in fp32 (gfx950 fp32 matrix instructions).
 //
 // The contract and the row layout are those of k_attn_prefix (attn_prefix.hip): a wave holds 32
-// packed query rows, a WG streams the keys of a split once for all of its rows, tile by tile through
-// two LDS buffers, and each (row, split) leaves a record.  Both contractions run on
-// v_mfma_f32_32x32x2_f32:
+// packed query rows, a WG streams the keys of a split once for all of its rows, and each (row, split)
+// leaves a record.  Both contractions run on v_mfma_f32_32x32x2_f32:
 //
 //   S^T[key][row] = K . Q^T    A = K rows (lane half hh holds half a row: one 16-byte LDS read feeds
 //                              four steps), B = the query row, in registers
 //   O^T[d][row]  += V^T . P^T  A = V from LDS (32 consecutive d of one key per half-wave), B = P^T,
 //                              the S^T accumulators as they are
+//
+// What bounds it: the fp32 matrix rate.  A wave's tile of 32 keys is d products of 64 clocks (3.9 us
+// at d = 128), far longer than its loads take: one LDS buffer per WG, and two WGs per CU, one of which
+// multiplies while the other loads.  (A tile's V requested during its scores and the next one's K
+// during its output measured 5 to 10 % slower; two accumulators in turn, no faster.)  1,024 rows of 8 KV
+// heads over 4,096 keys at d = 128, 180 us: 96 TFLOP/s of the 133 at that launch's clock (matrix pipe
+// busy 72 % of the CUs' time, by its counter).
 #include "attn_prefix.h"
 
 namespace td {
@@ -28,22 +34,19 @@ struct Prefix32Cfg {
   static constexpr int TILE = KEYS * D * 4;      // bytes of its K (or V) rows
   static constexpr int LOADS = TILE / 16 / THREADS;
   static_assert(TILE % (16 * THREADS) == 0, "a tile is a whole number of WG loads");
-  static constexpr int WAVES = 4 * TILE <= 64 * 1024 ? 2 : 1;  // per SIMD, as the LDS allows
+  static constexpr int WAVES = D <= 128 ? 2 : 1;  // per SIMD, as the registers allow
 };
 
 // Physical chunk of logical chunk c of key row r.  K: rotated by one chunk per row (the 16-byte reads
 // of 8 rows use different banks).  V: by 128 bytes for every other group of four rows (the two
 // half-waves read rows four apart).
 template <int CPR>
-__device__ inline int kchunk32(int r, int c) { return (c + r) % CPR; }
-template <int CPR>
 __device__ inline int vchunk32(int r, int c) { return (c + 8 * ((r >> 2) & 1)) % CPR; }
 
 template <int D, int RW, int KW>
 __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void k_attn_prefix32(DevState s, PrefixArgs a) {
   using C = Prefix32Cfg<D, RW, KW>;
-  __shared__ __attribute__((aligned(16))) unsigned char kbuf0[C::TILE], vbuf0[C::TILE];
-  __shared__ __attribute__((aligned(16))) unsigned char kbuf1[C::TILE], vbuf1[C::TILE];
+  __shared__ __attribute__((aligned(16))) unsigned char kbuf[C::TILE], vbuf[C::TILE];
   __shared__ int wred[4][RW];
   __shared__ float ml[KW == 2 ? RW * 128 : 1];
   const PrefixHdr p = *s.prefix;
@@ -83,34 +86,60 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
   const size_t page_rows = ((size_t)s.L * s.Hkv) << p.shift;
   const float* kpages = static_cast<const float*>(p.k);
   const float* vpages = static_cast<const float*>(p.v);
-  auto issue = [&](int tile, const TilePages& pg, unsigned char* kdst, unsigned char* vdst) __attribute__((always_inline)) {
-    const int tb = b0 + tile * C::KEYS;
+  // Load j of this thread writes 16-byte LDS chunk c = j THREADS + tid of the tile's K (and V): tile row
+  // c / CPR, whose logical chunk kchunk (vchunk) it fetches
+  auto geom = [&](int j, int t, int& r, int& kchunk, int& vchunk) __attribute__((always_inline)) {
+    const int c = j * C::THREADS + t, pc = c % C::CPR;
+    r = c / C::CPR;
+    kchunk = (pc + C::CPR - r % C::CPR) % C::CPR;
+    vchunk = (pc + C::CPR - 8 * ((r >> 2) & 1) % C::CPR) % C::CPR;
+  };
+  // (kept for a tile of consecutive rows, where there are registers for them)
+  constexpr bool kHold = C::LOADS <= 8 && D <= 128;
+  uint32_t kofs[kHold ? C::LOADS : 1], vofs[kHold ? C::LOADS : 1];
+  if constexpr (kHold) {
 #pragma unroll
     for (int j = 0; j < C::LOADS; ++j) {
-      int t = tid;
+      int r, kc, vc;
+      geom(j, tid, r, kc, vc);
+      kofs[j] = r * D + 4 * kc;
+      vofs[j] = r * D + 4 * vc;
+    }
+  }
+  auto load = [&](const float* src, unsigned char* dst, int j) __attribute__((always_inline)) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                     (__attribute__((address_space(3))) void*)(dst + (j * C::THREADS + wave * 64) * 16), 16, 0, 0);
+  };
+  auto issue = [&](int tile, const TilePages& pg) __attribute__((always_inline)) {
+    const int tb = b0 + tile * C::KEYS;
+    if (kHold && p.shift >= 6 && tb + C::KEYS <= hi) {  // (uniform) one page, no row past the end
+      const size_t row = (size_t)pg.p[0] * page_rows + head + (tb & ((1 << p.shift) - 1));
+#pragma unroll
+      for (int j = 0; j < C::LOADS; ++j) {
+        load(kpages + row * D + kofs[kHold ? j : 0], kbuf, j);
+        load(vpages + row * D + vofs[kHold ? j : 0], vbuf, j);
+      }
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < C::LOADS; ++j) {
+      int t = tid, r, kc, vc;
       asm volatile("" : "+v"(t));  // (the geometry is recomputed per load, not held)
-      const int c = j * C::THREADS + t, r = c / C::CPR, pc = c % C::CPR;
+      geom(j, t, r, kc, vc);
       const int n = min(tb + r, hi - 1);  // (rows past the end: the last row)
       const int e = p.shift >= 6 ? 0 : (n - (tb & ~63)) >> p.shift;
       const int page = e == 0 ? pg.p[0] : e == 1 ? pg.p[1] : e == 2 ? pg.p[2] : pg.p[3];
       const size_t row = (size_t)page * page_rows + head + (n & ((1 << p.shift) - 1));
-      const float* ks = kpages + row * D + (pc + C::CPR - r % C::CPR) % C::CPR * 4;
-      const float* vs = vpages + row * D + (pc + C::CPR - 8 * ((r >> 2) & 1) % C::CPR) % C::CPR * 4;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)ks,
-                                       (__attribute__((address_space(3))) void*)(kdst + (j * C::THREADS + wave * 64) * 16), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vs,
-                                       (__attribute__((address_space(3))) void*)(vdst + (j * C::THREADS + wave * 64) * 16), 16, 0, 0);
+      load(kpages + row * D + 4 * kc, kbuf, j);
+      load(vpages + row * D + 4 * vc, vbuf, j);
     }
   };
   auto pages_of = [&](int tile) __attribute__((always_inline)) { return tile_pages(p, (b0 + tile * C::KEYS) / 64); };
 
-  // the first two tiles go out before anything that waits for the tries
   TilePages next{};
   if (n_tiles > 0) {
-    const TilePages pg0 = pages_of(0), pg1 = pages_of(min(1, n_tiles - 1));
-    issue(0, pg0, kbuf0, vbuf0);
-    if (n_tiles > 1) issue(1, pg1, kbuf1, vbuf1);
-    if (n_tiles > 2) next = pages_of(2);
+    issue(0, pages_of(0));
+    if (n_tiles > 1) next = pages_of(1);
   }
   if (known) {
     prefix_row_keys(s, a, p, q);
@@ -124,24 +153,32 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[dt][v] = 0.0f;
 
-  auto step = [&](int tile, const unsigned char* kb, const unsigned char* vb, unsigned char* knext,
-                  unsigned char* vnext) __attribute__((always_inline)) {
-    // this thread's loads of the tile have landed, then every thread's, and the other buffer is free
-    // (the second tile is on its way already)
-    if (tile == 0 && n_tiles > 1) __builtin_amdgcn_s_waitcnt(wait_vm(2 * C::LOADS));
-    else __builtin_amdgcn_s_waitcnt(kWaitVmAll);
-    __syncthreads();
-    if (tile > 0 && tile + 1 < n_tiles) {
-      issue(tile + 1, next, knext, vnext);
-      if (tile + 2 < n_tiles) next = pages_of(tile + 2);
+  // operand reads: K rows rotated by their number (krot + k, less CPR past the end); V by 128 bytes for
+  // rows 4 .. 7, 12 .. 15, ..., which the second half-wave reads
+  const unsigned char* krow = kbuf + (kTile * kw + col) * (D * 4);
+  const uint32_t krot = (hh * (D / 8) + kTile * kw + col) % C::CPR;
+  const unsigned char* vrow = vbuf + (kTile * kw + 4 * hh) * (D * 4) + col * 4;
+  int voff[C::DT];
+#pragma unroll
+  for (int dt = 0; dt < C::DT; ++dt) voff[dt] = (dt + hh) % C::DT * 128;
+  auto vat = [&](int dt, int v) __attribute__((always_inline)) {  // key 8 (v / 4) + 4 hh + v % 4, element 32 dt + col
+    return *reinterpret_cast<const float*>(vrow + (8 * (v >> 2) + (v & 3)) * (D * 4) + voff[dt]);
+  };
+#pragma unroll 1
+  for (int tile = 0; tile < n_tiles; ++tile) {
+    if (tile > 0) {
+      __syncthreads();  // the tile before has been read
+      issue(tile, next);
+      if (tile + 1 < n_tiles) next = pages_of(tile + 1);
     }
+    __builtin_amdgcn_s_waitcnt(kWaitVmAll);
+    __syncthreads();
     const int tb = b0 + tile * C::KEYS + kTile * kw;  // this wave's 32 keys
-    if (tb >= span.hi || tb >= b1 || tb + kTile <= span.lo) return;  // (wave-uniform) no row sees them
+    if (tb >= span.hi || tb >= b1 || tb + kTile <= span.lo) continue;  // (wave-uniform) no row sees them
     // a score's sum over d: pieces of 32 products from a fresh accumulator, added up
     f32x16 acc;
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
-    const unsigned char* krow = kb + (kTile * kw + col) * (D * 4);
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       f32x16 piece;
@@ -149,7 +186,9 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
       for (int v = 0; v < 16; ++v) piece[v] = 0.0f;
 #pragma unroll
       for (int k = 4 * c; k < 4 * c + 4; ++k) {
-        const f32x4 kk = *reinterpret_cast<const f32x4*>(krow + kchunk32<C::CPR>(kTile * kw + col, hh * (D / 8) + k) * 16);
+        uint32_t at = krot + k;
+        asm volatile("" : "+v"(at));  // (the offsets are recomputed per tile, not held)
+        const f32x4 kk = *reinterpret_cast<const f32x4*>(krow + min(at, at - C::CPR) * 16);
 #pragma unroll
         for (int e = 0; e < 4; ++e) piece = __builtin_amdgcn_mfma_f32_32x32x2f32(kk[e], qv[k][e], piece, 0, 0, 0);
       }
@@ -184,12 +223,6 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[dt][v] *= alpha;
     }
-    // V of key 8 (v / 4) + 4 hh + v % 4, element 32 dt + col
-    const unsigned char* vrow = vb + kTile * kw * (D * 4) + (col & 3) * 4;
-    auto vat = [&](int dt, int v) __attribute__((always_inline)) {
-      const int r = 8 * (v >> 2) + 4 * hh + (v & 3);
-      return *reinterpret_cast<const float*>(vrow + r * (D * 4) + vchunk32<C::CPR>(r, 8 * dt + (col >> 2)) * 16);
-    };
     if (cut) {
       // a hidden key weighs 0, but 0 times an infinite or NaN V is NaN: such a tile adds its
       // products key by key, to the rows that see the key
@@ -211,13 +244,13 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
           for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
-              const f32x4 x = *reinterpret_cast<const f32x4*>(vb + (kTile * kw + i) * (D * 4) +
+              const f32x4 x = *reinterpret_cast<const f32x4*>(vbuf + (kTile * kw + i) * (D * 4) +
                                                               vchunk32<C::CPR>(i, 8 * dt + 2 * q4 + hh) * 16);
 #pragma unroll
               for (int e = 0; e < 4; ++e) o[dt][4 * q4 + e] += own ? wi * x[e] : 0.0f;
             }
         }
-        return;
+        continue;
       }
     }
     // (a tile's products from a fresh accumulator, then one addition: the rounding error of the
@@ -232,18 +265,14 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
 #pragma unroll
       for (int v = 0; v < 16; ++v) o[dt][v] += f[v];
     }
-  };
-  for (int t = 0; t < n_tiles; t += 2) {
-    step(t, kbuf0, vbuf0, kbuf1, vbuf1);
-    if (t + 1 < n_tiles) step(t + 1, kbuf1, vbuf1, kbuf0, vbuf0);
   }
 
+  __syncthreads();  // every wave has read its last tile
   if constexpr (KW == 2) {
-    // the second group hands its state over through LDS, lane by lane
-    static_assert(RW * 64 * (D / 4) * 4 <= C::TILE, "half of O fits a K buffer");
-    __syncthreads();
-    float* const o0 = reinterpret_cast<float*>(kbuf0);
-    float* const o1 = reinterpret_cast<float*>(kbuf1);
+    // the second group hands its state over through LDS, lane by lane: half of O in each buffer
+    static_assert(RW * 64 * (D / 4) * 4 <= C::TILE, "half of O fits a buffer");
+    float* const o0 = reinterpret_cast<float*>(kbuf);
+    float* const o1 = reinterpret_cast<float*>(vbuf);
     if (kw == 1) {
 #pragma unroll
       for (int x = 0; x < D / 4; ++x) {
@@ -255,25 +284,30 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
       ml[rw * 128 + 64 + lane] = lsum;
     }
     __syncthreads();
-    if (kw == 1) return;
-    const float m1 = ml[rw * 128 + lane], l1 = ml[rw * 128 + 64 + lane];
-    const float mn = fmaxf(m, m1);
-    const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(m1 - mn);
-    m = mn;
-    lsum = lsum * f0 + l1 * f1;
+    if (kw == 0) {
+      const float m1 = ml[rw * 128 + lane], l1 = ml[rw * 128 + 64 + lane];
+      const float mn = fmaxf(m, m1);
+      const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(m1 - mn);
+      m = mn;
+      lsum = lsum * f0 + l1 * f1;
 #pragma unroll
-    for (int x = 0; x < D / 4; ++x) {
-      const int at = (rw * (D / 4) + x) * 64 + lane, y = x + D / 4;
-      o[x / 16][x % 16] = o[x / 16][x % 16] * f0 + o0[at] * f1;
-      o[y / 16][y % 16] = o[y / 16][y % 16] * f0 + o1[at] * f1;
+      for (int x = 0; x < D / 4; ++x) {
+        const int at = (rw * (D / 4) + x) * 64 + lane, y = x + D / 4;
+        o[x / 16][x % 16] = o[x / 16][x % 16] * f0 + o0[at] * f1;
+        o[y / 16][y % 16] = o[y / 16][y % 16] * f0 + o1[at] * f1;
+      }
     }
+    __syncthreads();
   }
 
+  // two waves at a time: a buffer of 32 keys (or more) holds a wave's rows
   lsum += __shfl_xor(lsum, 32);
-  if constexpr (KW == 1) __syncthreads();  // every wave has read its last tile
-  // (a K or V buffer of 32 keys holds a wave's rows; beside the second group's O, the V buffers do)
-  unsigned char* const mine = KW == 2 ? (rw == 0 ? vbuf0 : vbuf1) : rw == 0 ? kbuf0 : rw == 1 ? vbuf0 : rw == 2 ? kbuf1 : vbuf1;
-  prefix_output<float, D>(s, a, u, q, lane, m, lsum, o, reinterpret_cast<float*>(mine));
+#pragma unroll
+  for (int turn = 0; turn < RW; turn += 2) {
+    if (turn > 0) __syncthreads();
+    if (kw == 0 && rw / 2 * 2 == turn)
+      prefix_output<float, D>(s, a, u, q, lane, m, lsum, o, reinterpret_cast<float*>(rw % 2 ? vbuf : kbuf));
+  }
 }
 
 template <int D>

@@ -90,7 +90,7 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   a.row_blocks = (int)((rows + rpb - 1) / rpb);
   const long keys = s.W > 0 ? std::min(c->prefix_length, s.W) : c->prefix_length;
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * s.T * qn * s.Hq));
-  a.splits = prefix_splits((long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
+  a.splits = prefix_splits(s, (long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
   a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
   *splits = a.splits;
   return launch_prefix(s, a, st, ev0, nullptr);
@@ -266,7 +266,7 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
   a.row_blocks = (int)((rows + rpb - 1) / rpb);
   const long keys = s.W > 0 ? std::min(pos + n, s.W) : pos + n;
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * n * s.Hq));
-  a.splits = td::prefix_splits((long)n_layers * s.Hkv * a.row_blocks, keys, std::max(1l, fit));
+  a.splits = td::prefix_splits(s, (long)n_layers * s.Hkv * a.row_blocks, keys, std::max(1l, fit));
   a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
   a.part_o = a.splits > 1 ? c->prefix_o : nullptr;
   a.part_ml = c->prefix_ml;

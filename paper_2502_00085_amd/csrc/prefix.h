@@ -32,7 +32,7 @@ struct PrefixArgs {
 // Query rows of a workgroup for a pass of this many rows per KV head.
 int prefix_rows_per_block(const DevState& s, long rows);
 // Splits of `keys` keys for `units` (layer, KV head, row block) units, at most `most`.
-int prefix_splits(long units, long keys, long most);
+int prefix_splits(const DevState& s, long units, long keys, long most);
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
                            hipEvent_t ev1);
