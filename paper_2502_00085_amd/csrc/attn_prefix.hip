@@ -140,12 +140,7 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     }
   };
 
-  // (what waits for the tries comes first: loads return in order, and these must not wait for tiles)
-  if (known) {
-    prefix_row_keys(s, a, p, q);
-    span = prefix_span(q);
-  }
-  // the first two tiles
+  // the first two tiles go out before anything that waits for the tries
   TilePages next{};
   if (t0 < t1) {
     const bool main = m0 < m1;
@@ -155,6 +150,10 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     issue(x0, pg0, kbuf0, vbuf0);
     if (two) issue(x1, pg1, kbuf1, vbuf1);
     if (m0 + 2 < m1) next = tile_pages(p, m0 + 2);
+  }
+  if (known) {
+    prefix_row_keys(s, a, p, q);
+    span = prefix_span(q);
   }
   const int grp = lane >> 4, tm = (lane & 15) >> 2, tq = lane & 3;
   int kread[C::KSTEPS], vread[C::VROT][C::DT];
