@@ -182,7 +182,7 @@ __device__ inline void prefix_output(const DevState& s, const PrefixArgs& a, con
   // where the row goes: its record, or its row of out (-1: nowhere)
   int64_t at = -1;
   if (record) {
-    at = (((int64_t)u.li * a.tries * a.per_trie + q.owner) * s.Hq + u.g * G + q.head) * a.splits + u.split;
+    at = (((int64_t)u.li * a.tries * a.per_trie + q.owner) * s.Hq + u.g * G + q.head) * a.records + u.split;
     if (q.in && hh == 0) a.part_ml[at] = make_float2(some ? m : kPrefixNegBig, some ? lsum : 0.0f);
     if (!some) at = -1;
   } else if (q.in) {

@@ -14,6 +14,7 @@
 // four smaller ones, whose numbers are loaded a tile ahead by scalar loads.
 #include <algorithm>
 
+#include "attn_common.h"
 #include "attn_prefix.h"
 
 namespace td {
@@ -40,7 +41,11 @@ struct PrefixCfg {
   static constexpr int VROT = 8 % NBLK == 0 ? 1 : 4;  // rotations of V rows 8 apart
 };
 
-template <int D, int RW, int KW>
+// TRIES: the launch's last WGs take the tries' own nodes (PrefixArgs::trie_splits), for calls so small
+// that a launch of their own would run after this one instead of beside it.  A trie's rows in its
+// pool are one page of nodes; every live row sees its shared prefix, and of the nodes after it those
+// whose ancestor mask holds the row's beam.
+template <int D, int RW, int KW, bool TRIES>
 __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k_attn_prefix(DevState s, PrefixArgs a) {
   using C = PrefixCfg<D, RW, KW>;
   static_assert(2 * C::LOADS < 64, "the wait counter holds a tile's loads");
@@ -52,16 +57,47 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   __shared__ __attribute__((aligned(16))) unsigned char kbuf1[2 * C::HALF], vbuf1[2 * C::HALF];
   __shared__ int wred[4][RW];
   __shared__ float ml[KW == 2 ? RW * 128 : 1];
-  const PrefixHdr p = *s.prefix;
-  const PrefixUnit u = prefix_unit(s, a);
-  const int lab = a.layer_begin + u.li;
+  PrefixHdr p = *s.prefix;
+  const bool trie = TRIES && blockIdx.x >= a.prefix_wgs;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW;
   const int col = lane & 31, hh = lane >> 5;
 
-  const int r0 = u.rb * RW * 32;
-  PrefixRow q = prefix_row(s, a, u.li, r0 + rw * 32 + col);
+  PrefixUnit u;
+  PrefixRow q;
+  TrieHdr th{};
+  int t = 0, r0, share, shares;  // (of the keys)
+  if (TRIES && trie) {
+    int x = blockIdx.x - a.prefix_wgs;
+    shares = a.trie_splits;
+    share = x % shares;
+    x /= shares;
+    u.rb = x % a.trie_blocks;
+    x /= a.trie_blocks;
+    u.g = x % s.Hkv;
+    x /= s.Hkv;
+    t = x % a.tries;
+    u.li = x / a.tries;
+    u.split = a.splits + share;
+    th = s.hdr[t];
+    r0 = u.rb * RW * 32;
+    const int G = s.Hq / s.Hkv, r = r0 + rw * 32 + col, i = r / G;
+    q.in = i < a.per_trie;
+    q.t = t;
+    q.j = q.in ? i : 0;
+    q.head = r % G;
+    q.owner = t * a.per_trie + q.j;
+    q.at = ((size_t)u.li * a.tries + t) * a.q_stride + q.j;
+    q.lo = q.hi = 0;
+  } else {
+    u = prefix_unit(s, a);
+    share = u.split;
+    shares = a.splits;
+    r0 = u.rb * RW * 32;
+    q = prefix_row(s, a, u.li, r0 + rw * 32 + col);
+  }
+  const int lab = a.layer_begin + u.li;
   // the lane's query row as B operands of S^T: half hh of its d range (loaded before anything is known
   // of the row; a row that sees nothing has no say)
   bf16x8 qv[C::KSTEPS];
@@ -72,7 +108,15 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     for (int k = 0; k < C::KSTEPS; ++k) qv[k] = __builtin_bit_cast(bf16x8, qp[k]);
   }
   PrefixSpan span, all;  // (of the wave; of the WG)
-  const bool known = prefix_range(s, a, p, r0, RW * 32, &all);
+  bool known = true;
+  if (TRIES && trie) {
+    const int lo = window_lo(s, t, th.base, th.n_nodes, th.leaf_depth, wred[0]);
+    __syncthreads();
+    const int shared = max(lo, min(th.n_shared, th.n_nodes));
+    all = {lo, th.n_nodes, lo, shared};
+  } else {
+    known = prefix_range(s, a, p, r0, RW * 32, &all);
+  }
   if (!known) {  // a window: from the rows' positions
     prefix_row_keys(s, a, p, q);
     span = prefix_span(q);
@@ -81,17 +125,25 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   const int lo = all.lo, hi = all.hi;
   // tiles of 64 keys, at multiples of 64: this split's share
   const int first = hi > 0 ? lo / 64 : 0, tiles = hi > 0 ? (hi + 63) / 64 - first : 0;
-  const int per = (tiles + a.splits - 1) / a.splits;
-  const int t0 = first + u.split * per, t1 = max(t0, min(first + tiles, t0 + per));
+  const int per = (tiles + shares - 1) / shares;
+  const int t0 = first + share * per, t1 = max(t0, min(first + tiles, t0 + per));
   // of it [m0, m1): tiles that every row sees whole; the cut ones before and after
   const int m0 = min(max(t0, (all.all_lo + 63) / 64), t1), m1 = max(m0, min(t1, all.all_hi / 64));
   const int before = m0 - t0, cut = before + t1 - m1;
   auto cut_tile = [&](int i) __attribute__((always_inline)) { return i < before ? t0 + i : m1 + i - before; };
 
-  const size_t head = ((size_t)lab * s.Hkv + u.g) << p.shift;  // rows before this (layer, KV head) in a page
-  const size_t page_rows = ((size_t)s.L * s.Hkv) << p.shift;
+  size_t head = ((size_t)lab * s.Hkv + u.g) << p.shift;  // rows before this (layer, KV head) in a page
+  size_t page_rows = ((size_t)s.L * s.Hkv) << p.shift;
   const __bf16* kpages = static_cast<const __bf16*>(p.k);
   const __bf16* vpages = static_cast<const __bf16*>(p.v);
+  if (TRIES && trie) {  // (one page)
+    p.shift = 30;
+    head = pool_row(s, t, lab, u.g, th.base) / D;
+    page_rows = 0;
+    kpages = static_cast<const __bf16*>(s.k_pool);
+    vpages = static_cast<const __bf16*>(s.v_pool);
+  }
+  auto pages_of = [&](int tile) __attribute__((always_inline)) { return TRIES && trie ? TilePages{} : tile_pages(p, tile); };
 
   // Load j of this thread writes 16-byte LDS chunk c = j THREADS + tid of the tile's K (and V): tile
   // row c / CPR at physical chunk c % CPR; K rows rotated by one chunk per row, V rows by one 64-byte
@@ -146,12 +198,19 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     const bool main = m0 < m1;
     const int x0 = main ? m0 : cut_tile(0), x1 = main ? m0 + 1 : cut_tile(1);
     const bool two = main ? m0 + 1 < m1 : cut > 1;
-    const TilePages pg0 = tile_pages(p, x0), pg1 = tile_pages(p, two ? x1 : x0);
+    const TilePages pg0 = pages_of(x0), pg1 = pages_of(two ? x1 : x0);
     issue(x0, pg0, kbuf0, vbuf0);
     if (two) issue(x1, pg1, kbuf1, vbuf1);
-    if (m0 + 2 < m1) next = tile_pages(p, m0 + 2);
+    if (m0 + 2 < m1) next = pages_of(m0 + 2);
   }
-  if (known) {
+  if (TRIES && trie) {
+    if (q.in && q.j < th.n_live) {
+      q.lo = all.lo;
+      q.hi = all.hi;
+    }
+    span = prefix_span(q);
+    span.all_hi = min(span.all_hi, all.all_hi);
+  } else if (known) {
     prefix_row_keys(s, a, p, q);
     span = prefix_span(q);
   }
@@ -235,7 +294,7 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     __syncthreads();
     if (tile > m0 && tile + 1 < m1) {
       issue(tile + 1, next, knext, vnext);
-      if (tile + 2 < m1) next = tile_pages(p, tile + 2);
+      if (tile + 2 < m1) next = pages_of(tile + 2);
     }
     f32x16 acc[NH];
 #pragma unroll
@@ -264,10 +323,16 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   for (int i = 0; i < cut; i += 2) {
     if (i > 0 || m0 < m1) {
       const bool two = i + 1 < cut;
-      const TilePages pg0 = tile_pages(p, cut_tile(i)), pg1 = tile_pages(p, cut_tile(two ? i + 1 : i));
+      const TilePages pg0 = pages_of(cut_tile(i)), pg1 = pages_of(cut_tile(two ? i + 1 : i));
       __syncthreads();  // both buffers are free
       issue(cut_tile(i), pg0, kbuf0, vbuf0);
       if (two) issue(cut_tile(i + 1), pg1, kbuf1, vbuf1);
+    }
+    uint64_t masks[2] = {0, 0};  // (of a trie's nodes) of key `lane` of either tile
+    if (TRIES && trie) {
+      const uint64_t* mp = s.mask + (size_t)t * s.cap + th.base;
+      masks[0] = mp[min(cut_tile(i) * 64 + lane, hi - 1)];
+      masks[1] = mp[min(cut_tile(min(i + 1, cut - 1)) * 64 + lane, hi - 1)];
     }
     __builtin_amdgcn_s_waitcnt(kWaitVmAll);
     __syncthreads();
@@ -286,11 +351,19 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
         acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kh + kread[k]), qv[k], acc, 0, 0, 0);
       bf16x8 pb[2];
       const bool whole = hb >= span.all_lo && hb + 32 <= span.all_hi;  // (wave-uniform)
+      const uint64_t mk = h < 2 ? masks[0] : masks[1];
+      const int mlo = (int)(uint32_t)mk, mhi = (int)(uint32_t)(mk >> 32);
       if (!whole) {  // hidden scores become -inf
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          const int n = hb + 8 * (v >> 2) + 4 * hh + (v & 3);
-          acc[v] = ((n >= q.lo) & (n < q.hi)) ? acc[v] : -INFINITY;
+          const int i32 = 8 * (v >> 2) + 4 * hh + (v & 3), n = hb + i32;
+          bool ok = (n >= q.lo) & (n < q.hi);
+          if (TRIES && trie) {
+            const int at = (32 * (h & 1) + i32) << 2;
+            const uint32_t w0 = (uint32_t)__builtin_amdgcn_ds_bpermute(at, mlo), w1 = (uint32_t)__builtin_amdgcn_ds_bpermute(at, mhi);
+            ok &= (((q.j < 32 ? w0 : w1) >> (q.j & 31)) & 1u) != 0;
+          }
+          acc[v] = ok ? acc[v] : -INFINITY;
         }
       }
       weigh(acc, pb);
@@ -318,7 +391,12 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
 #pragma unroll
         for (int v = 0; v < 16; ++v) w = v == vi ? (float)pb[v >> 3][v & 7] : w;
         w = __shfl(w, col + 32 * ((n >> 2) & 1));
-        const bool own = hb + n >= q.lo && hb + n < q.hi;
+        bool own = hb + n >= q.lo && hb + n < q.hi;
+        if (TRIES && trie) {
+          const int at = 32 * (h & 1) + n;
+          const uint32_t w0 = (uint32_t)__builtin_amdgcn_readlane(mlo, at), w1 = (uint32_t)__builtin_amdgcn_readlane(mhi, at);
+          own = own && (((q.j < 32 ? w0 : w1) >> (q.j & 31)) & 1u) != 0;
+        }
 #pragma unroll
         for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
@@ -369,12 +447,20 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
 
 template <int D>
 void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
-  const dim3 grid(a.n_layers * s.Hkv * a.splits * a.row_blocks);
-#define LAUNCH_PREFIX(RW, KW) \
-  hipExtLaunchKernelGGL((k_attn_prefix<D, RW, KW>), grid, dim3(64 * RW * KW), 0, st, ev0, ev1, 0, s, a)
-  if (rpb == 32) LAUNCH_PREFIX(1, 2);
-  else if (rpb == 64) LAUNCH_PREFIX(2, 2);
-  else LAUNCH_PREFIX(4, 1);
+  const dim3 grid(a.n_layers * s.Hkv * (a.splits * a.row_blocks + a.tries * a.trie_blocks * a.trie_splits));
+#define LAUNCH_PREFIX(RW, KW, TRIES) \
+  hipExtLaunchKernelGGL((k_attn_prefix<D, RW, KW, TRIES>), grid, dim3(64 * RW * KW), 0, st, ev0, ev1, 0, s, a)
+  if constexpr (D == 64 || D == 96 || D == 128) {
+    if (a.trie_splits > 0) {
+      if (rpb == 32) LAUNCH_PREFIX(1, 2, true);
+      else if (rpb == 64) LAUNCH_PREFIX(2, 2, true);
+      else LAUNCH_PREFIX(4, 1, true);
+      return;
+    }
+  }
+  if (rpb == 32) LAUNCH_PREFIX(1, 2, false);
+  else if (rpb == 64) LAUNCH_PREFIX(2, 2, false);
+  else LAUNCH_PREFIX(4, 1, false);
 #undef LAUNCH_PREFIX
 }
 
@@ -489,6 +575,7 @@ int prefix_splits(const DevState& s, long units, long keys, long most) {
 
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
   const int rpb = prefix_rows_per_block(s, (long)a.tries * a.per_trie * (s.Hq / s.Hkv));
+  if (a.trie_splits > 0 && (a.rows != PrefixRows::kLeaves || s.dtype != TD_BF16 || !mfma_head_dim(s.D))) return hipErrorInvalidValue;
   if (s.dtype == TD_F32) return launch_prefix32(s, a, rpb, st, ev0, ev1);
   switch (s.D) {
 #define PREFIX_CASE(DD) case DD: launch_d<DD>(s, a, rpb, st, ev0, ev1); break;

@@ -203,8 +203,15 @@ hipError_t attn_layers(td_ctx* c, int layer_begin, int n_layers, const void* d_q
   if (!a.moves && !rows_copied) e = td::copy_due_rows(c, layer_begin, n_layers, st, mv0, mv1);
   const bool prefix = c->prefix_length > 0;
   int prefix_splits = 0;
-  if (e == hipSuccess && prefix)
-    e = td::prefix_pass(c, false, layer_begin, n_layers, 0, s.b, s.b, nullptr, d_q, scale_log2, 64, st, ev0, &prefix_splits);
+  bool tries = false;
+  if (e == hipSuccess && prefix) {
+    // (leaves to store, rows to move or a forced split count: the tries' launch does that)
+    const bool beside = mfma && !a.kv_pending && !a.moves && c->splits_override == 0;
+    e = td::prefix_pass(c, false, layer_begin, n_layers, 0, s.b, s.b, nullptr, d_q, scale_log2, 64, beside ? nodes : 0, st, ev0,
+                        &prefix_splits, &tries);
+  }
+  a.prefix_tries = tries;
+  if (tries) return e == hipSuccess ? td::prefix_merge(c, false, a, prefix_splits, rpb, s.b, st, ev1) : e;
   const bool fold = prefix && td::prefix_fold(c, a, prefix_splits);
   a.partial = a.splits > 1 || (prefix && !fold);
   if (e == hipSuccess) e = td::launch_attn(kernel, s, a, st, prefix ? nullptr : ev0, a.partial ? nullptr : ev1);
@@ -462,8 +469,9 @@ td_status trie_tree_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32
         hipEvent_t first = l == 0 && q0 == 0 ? ev0 : nullptr;
         if (prefix) {
           // (few splits: every row merges their records by itself, one after the other)
-          e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, q0, a.qn, q_max, d_qslots, a.q, a.scale_log2, 8, st, first,
-                              &a.prefix_splits);
+          bool tries;
+          e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, q0, a.qn, q_max, d_qslots, a.q, a.scale_log2, 8, 0, st, first,
+                              &a.prefix_splits, &tries);
           a.prefix_o = c->prefix_o;
           a.prefix_ml = c->prefix_ml;
           first = nullptr;
@@ -493,9 +501,10 @@ td_status trie_tree_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32
     a.xcd_group = a.row_blocks > 1 && ((long)s.T * a.n_layers * s.Hkv * a.splits) % 8 == 0 ? 1 : 0;
     a.partial = a.splits > 1 || prefix;
       int prefix_splits = 0;
+    bool tries = false;
     if (prefix)
-      e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, 0, q_max, q_max, d_qslots, a.q, a.scale_log2, 64, st, first,
-                          &prefix_splits);
+      e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, 0, q_max, q_max, d_qslots, a.q, a.scale_log2, 64, 0, st, first,
+                          &prefix_splits, &tries);
     const bool fold = prefix && td::prefix_fold(c, a, prefix_splits);
     a.partial = a.splits > 1 || (prefix && !fold);
     if (e == hipSuccess) e = td::launch_attn_mfma(ds, a, st, prefix ? nullptr : first, a.partial ? nullptr : last);

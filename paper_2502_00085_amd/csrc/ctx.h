@@ -51,11 +51,12 @@ void note_written(td_ctx* c, int layer_begin, int n_layers);
 hipError_t copy_due_rows(td_ctx* c, int layer_begin, int n_layers, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1);
 
 // The pass over the shared prefix for the tries' rows (prefix.cpp): leaves (q_max = b, no qslots) or
-// stored nodes (queries q0 .. q0 + qn - 1 of each trie), at most max_splits splits.  Returns the splits
-// of its records.
+// stored nodes (queries q0 .. q0 + qn - 1 of each trie), at most max_splits splits.  trie_nodes > 0, a
+// bound on the nodes of any trie whose rows are all stored: it may take the tries' own nodes too
+// (*tries).  *splits: its records per row.
 hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int q0, int qn, int q_max,
-                       const int32_t* d_qslots, const void* d_q, float scale_log2, int max_splits, hipStream_t st,
-                       hipEvent_t ev0, int* splits);
+                       const int32_t* d_qslots, const void* d_q, float scale_log2, int max_splits, long trie_nodes,
+                       hipStream_t st, hipEvent_t ev0, int* splits, bool* tries);
 // Whether an unsplit attention launch merges that many splits of records into its output itself (a:
 // gets the records), which saves its partials and a launch.
 bool prefix_fold(const td_ctx* c, AttnArgs& a, int splits);

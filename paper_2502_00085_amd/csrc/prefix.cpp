@@ -16,6 +16,9 @@ namespace {
 // Records an attention launch merges by itself, one after the other: more are merged by a launch of
 // their own, eight at a time.
 constexpr int kFoldSplits = 4;
+constexpr long kOneRound = 512;  // WGs of a pass that run at once (two per CU)
+constexpr long kTrieTiles = 8;
+constexpr long kShortPass = 16;  // tiles of the prefix per WG
 constexpr size_t kWorkFloats = 16u << 20;  // of either workspace, unless one layer needs more
 
 td_status bad_layers(td_ctx* c, int layer_begin, int n_layers) {
@@ -69,8 +72,8 @@ td_status store_args(td_ctx* c, const td_rope* rope, const void* q, int64_t qs, 
 namespace td {
 
 hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int q0, int qn, int q_max,
-                       const int32_t* d_qslots, const void* d_q, float scale_log2, int max_splits, hipStream_t st,
-                       hipEvent_t ev0, int* splits) {
+                       const int32_t* d_qslots, const void* d_q, float scale_log2, int max_splits, long trie_nodes,
+                       hipStream_t st, hipEvent_t ev0, int* splits, bool* tries) {
   const DevState& s = c->dev;
   PrefixArgs a{};
   a.q = d_q;
@@ -92,7 +95,25 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * s.T * qn * s.Hq));
   a.splits = prefix_splits(s, (long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
   a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
-  *splits = a.splits;
+  a.records = a.splits;
+  *tries = false;
+  if (trie_nodes > 0) {
+    // the tries' own nodes in the same launch, where all of its WGs run at once, none has more than
+    // kTrieTiles tiles of a trie, and the pass itself is short.  A step of 4 x 8 beams over 4,096 positions
+    // and 272 nodes each, a layer: 22.3 us, with a launch of its own for the tries 29.5; 2 x 4 beams over
+    // 50,001 positions (32 KV heads, 49 tiles per WG): 123.5 and 120.8.
+    const long wgs = (long)n_layers * s.Hkv * a.row_blocks * a.splits, tiles = (trie_nodes + 63) / 64;
+    const long blocks = (qn * (s.Hq / s.Hkv) + rpb - 1) / rpb, units = (long)n_layers * s.T * s.Hkv * blocks;
+    const long ts = std::max(1l, std::min({(tiles + 1) / 2, 256 / units, fit - a.splits}));
+    if (wgs + units * ts <= kOneRound && (keys + 63) / 64 <= (long)kShortPass * a.splits && (tiles + ts - 1) / ts <= kTrieTiles && a.splits + ts <= fit) {
+      a.trie_splits = (int)ts;
+      a.trie_blocks = (int)blocks;
+      a.prefix_wgs = (uint32_t)wgs;
+      a.records = a.splits + a.trie_splits;
+      *tries = true;
+    }
+  }
+  *splits = a.records;
   return launch_prefix(s, a, st, ev0, nullptr);
 }
 
@@ -111,7 +132,7 @@ hipError_t prefix_merge(td_ctx* c, bool nodes, const AttnArgs& a, int splits, in
   m.prefix_o = c->prefix_o;
   m.prefix_ml = c->prefix_ml;
   m.prefix_splits = splits;
-  m.trie = c->prefix_trie_part;
+  m.trie = a.prefix_tries ? nullptr : c->prefix_trie_part;
   m.trie_splits = a.splits;
   m.block_rows = block_rows;
   m.row_blocks = a.row_blocks32;
@@ -266,7 +287,7 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
   a.row_blocks = (int)((rows + rpb - 1) / rpb);
   const long keys = s.W > 0 ? std::min(pos + n, s.W) : pos + n;
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * n * s.Hq));
-  a.splits = td::prefix_splits(s, (long)n_layers * s.Hkv * a.row_blocks, keys, std::max(1l, fit));
+  a.records = a.splits = td::prefix_splits(s, (long)n_layers * s.Hkv * a.row_blocks, keys, std::max(1l, fit));
   a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
   a.part_o = a.splits > 1 ? c->prefix_o : nullptr;
   a.part_ml = c->prefix_ml;

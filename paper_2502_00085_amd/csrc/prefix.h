@@ -12,7 +12,7 @@ enum class PrefixRows { kLeaves, kNodes, kChunk };
 // One pass over the prefix.  Row owner o in [0, tries * per_trie) is query q0 + o % per_trie of trie
 // o / per_trie (kChunk: one "trie", whose query j sits at position pos0 + j); a row is a (owner,
 // query head of one KV head) pair.  Each (row, split) leaves a record, number ((li * owners + o) * Hq +
-// head) * splits + split: D floats O at part_o, the shift m (log2 domain) and the sum l at part_ml.  A
+// head) * records + split: D floats O at part_o, the shift m (log2 domain) and the sum l at part_ml.  A
 // record with l = 0 (no key of the split) has no O.
 struct PrefixArgs {
   const void* q;                    // [n_layers][tries][q_stride][Hq][D]
@@ -26,7 +26,12 @@ struct PrefixArgs {
   int pos0 = 0;                     // (kChunk)
   float scale_log2;
   int row_blocks = 1, splits = 1;
+  int records = 1;                  // per row: splits, and after them trie_splits
   int xcd_group = 0;                // row blocks of one (layer, KV head, split) on one XCD
+  // (kLeaves, bf16) the same launch takes the tries' own nodes too, all of which are stored: after
+  // prefix_wgs WGs come those of (layer, trie, KV head, block of a trie's rows, split of its nodes)
+  int trie_splits = 0, trie_blocks = 0;
+  uint32_t prefix_wgs = 0;
 };
 
 // Query rows of a workgroup for a pass of this many rows per KV head.

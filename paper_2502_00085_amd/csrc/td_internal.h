@@ -132,6 +132,7 @@ struct AttnArgs {
   const float* prefix_o = nullptr;
   const float2* prefix_ml = nullptr;
   int prefix_splits = 0;
+  int prefix_tries = 0;            // 1: those records hold the tries' own nodes too (no launch for them)
   // (prefill-shaped tree kernels beside a prefix) the launch's queries, q0 .. q0 + qn - 1 of each trie
   int q0 = 0, qn = 0;
   int half_wgs = 0;                // (matrix-core kernel) 1: 4-wave WGs, two per CU (two row blocks:
