@@ -24,8 +24,9 @@
  *
  * Memory.  The caller owns every tensor (K/V pools, queries, outputs, logits and
  * selections) as device memory; PyTorch tensors are the intended source.  The library
- * owns only the trie metadata and a fixed workspace, both allocated in td_create.  The
- * three hot calls allocate nothing, never synchronise the host, and are ordered by the
+ * owns only the trie metadata and a fixed workspace, both allocated in td_create (and, with a
+ * shared prefix, its page table and a workspace, allocated in td_set_prefix).  The
+ * hot calls allocate nothing, never synchronise the host, and are ordered by the
  * stream they are given.  One context is driven by one stream at a time.
  *
  * Layouts (row-major, innermost index last; "cap" = desc.capacity):
@@ -214,8 +215,8 @@ typedef struct {
   int32_t interleaved;  /* 0: pair i is elements (i, i + dim / 2); 1: (2i, 2i + 1)                  */
 } td_rope;
 
-/* Store n tokens of the prefix at positions pos .. pos + n - 1 (inside the table; `length` plays no
- * part), for layers [layer_begin, +n_layers): K rotated to its position (rope NULL: as it is) and V
+/* Store n <= 2^26 tokens of the prefix at positions pos .. pos + n - 1 (inside the table; `length`
+ * plays no part), for layers [layer_begin, +n_layers): K rotated to its position (rope NULL: as it is) and V
  * go to their pages, q rotated to q_out.  Either of (q, q_out) and (k, v) may be NULL; q_out may be
  * q.  Rows [nl][n][heads][d], where consecutive rows lie q_stride (k_stride, v_stride) elements
  * apart - a slice of a fused projection's output does - at least heads * d and a multiple of 8;
@@ -235,7 +236,8 @@ td_status trie_prefix_attn(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, i
 
 /* Store rows of the tries' nodes, for layers [layer_begin, +n_layers): K rotated to the node's
  * position, S + its depth (S = 0 without a prefix; rope NULL: as it is), and V go to the node's pool
- * row, q rotated to q_out.  Arguments as in trie_prefix_store, rows [nl][T][q_max][heads][d].
+ * row, q rotated to q_out.  Arguments as in trie_prefix_store, rows [nl][T][q_max][heads][d],
+ * T * q_max <= 2^26.
  *   d_qslots [T][q_max] (device): the nodes by logical slot, as in trie_tree_attn (a prefill, or
  *   draft nodes).  A row with no node (-1, or a slot past the last) stores nothing, and its q_out is
  *   zero.  The slots of one trie must be distinct when K/V are given (else which row's chunks a node

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <new>
 #include <vector>
 
 #include "ctx.h"
@@ -19,11 +20,21 @@ constexpr int kFoldSplits = 4;
 constexpr long kOneRound = 512;  // WGs of a pass that run at once (two per CU)
 constexpr long kTrieTiles = 8;
 constexpr long kShortPass = 16;  // tiles of the prefix per WG
+constexpr int kStoreRows = 1 << 26;  // rows per layer of a store (what a launch's grid holds)
 constexpr size_t kWorkFloats = 16u << 20;  // of either workspace, unless one layer needs more
 
 td_status bad_layers(td_ctx* c, int layer_begin, int n_layers) {
   if (n_layers < 1 || layer_begin < 0 || n_layers > c->dev.L || layer_begin > c->dev.L - n_layers)
     return fail(c, TD_EINVAL, "layer range [%d, +%d) outside [0, %d)", layer_begin, n_layers, c->dev.L);
+  return TD_OK;
+}
+
+// The context's device is the current one (its memory is there, and so are the kernels).
+td_status other_device(td_ctx* c) {
+  int d = 0;
+  const hipError_t e = hipGetDevice(&d);
+  if (e != hipSuccess) return hip_fail(c, e, "hipGetDevice");
+  if (d != c->device) return fail(c, TD_EINVAL, "the context lives on device %d, the current one is %d", c->device, d);
   return TD_OK;
 }
 
@@ -148,9 +159,7 @@ hipError_t prefix_merge(td_ctx* c, bool nodes, const AttnArgs& a, int splits, in
 
 extern "C" {
 
-td_status td_set_prefix(td_ctx* c, const td_prefix* d) {
-  if (!c) return TD_EINVAL;
-  c->err.clear();
+static td_status set_prefix(td_ctx* c, const td_prefix* d) {
   const td::DevState& s = c->dev;
   td::PrefixHdr h;
   std::vector<int32_t> table;
@@ -164,14 +173,14 @@ td_status td_set_prefix(td_ctx* c, const td_prefix* d) {
     const int64_t room = (int64_t)d->n_table * d->page_size;
     if (room > (1 << 30)) return fail(c, TD_EINVAL, "the page table holds more than 2^30 positions");
     if (d->length < 0 || d->length > room) return fail(c, TD_EINVAL, "prefix length must be in [0, n_table * page_size]");
-    std::vector<uint8_t> used(d->n_pages, 0);
-    for (int32_t i = 0; i < d->n_table; ++i) {
-      const int32_t page = d->h_page_table[i];
-      if (page < 0 || page >= d->n_pages) return fail(c, TD_EINVAL, "page table entry %d: page %d outside [0, %d)", i, page, d->n_pages);
-      if (used[page]) return fail(c, TD_EINVAL, "page table entry %d: page %d is listed twice", i, page);
-      used[page] = 1;
-    }
     table.assign(d->h_page_table, d->h_page_table + d->n_table);
+    for (int32_t i = 0; i < d->n_table; ++i)
+      if (table[i] < 0 || table[i] >= d->n_pages)
+        return fail(c, TD_EINVAL, "page table entry %d: page %d outside [0, %d)", i, table[i], d->n_pages);
+    std::vector<int32_t> sorted(table);
+    std::sort(sorted.begin(), sorted.end());
+    const auto twice = std::adjacent_find(sorted.begin(), sorted.end());
+    if (twice != sorted.end()) return fail(c, TD_EINVAL, "page table: page %d is listed twice", *twice);
     table.insert(table.end(), td::kPrefixTablePad, table[0]);
     h.k = d->k_pages;
     h.v = d->v_pages;
@@ -179,6 +188,7 @@ td_status td_set_prefix(td_ctx* c, const td_prefix* d) {
     h.room = (int32_t)room;
     while ((1 << h.shift) < d->page_size) ++h.shift;
   }
+  if (td_status r = other_device(c)) return r;
   hipError_t e = hipDeviceSynchronize();
   if (d) {
     if (e == hipSuccess && table.size() > c->prefix_table_cap) {
@@ -209,6 +219,16 @@ td_status td_set_prefix(td_ctx* c, const td_prefix* d) {
   return TD_OK;
 }
 
+td_status td_set_prefix(td_ctx* c, const td_prefix* d) {
+  if (!c) return TD_EINVAL;
+  c->err.clear();
+  try {
+    return set_prefix(c, d);
+  } catch (const std::bad_alloc&) {  // (the table's copy)
+    return fail(c, TD_EINVAL, "out of host memory for the page table");
+  }
+}
+
 td_status trie_prefix_store(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n, const td_rope* rope,
                             const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v,
                             int64_t v_stride, void* d_q_out, hipStream_t st) {
@@ -220,6 +240,8 @@ td_status trie_prefix_store(td_ctx* c, int32_t layer_begin, int32_t n_layers, in
   if (!c->prefix) return fail(c, TD_ESTATE, "no prefix is attached (td_set_prefix)");
   if (n < 1 || pos < 0 || n > c->prefix_room || pos > c->prefix_room - n)
     return fail(c, TD_EINVAL, "positions [%d, +%d) outside the prefix's %d", pos, n, c->prefix_room);
+  if (n > kStoreRows) return fail(c, TD_EINVAL, "n must be at most 2^26");
+  if (td_status r = other_device(c)) return r;
   a.rows = td::PrefixRows::kChunk;
   a.layer_begin = layer_begin;
   a.n_layers = n_layers;
@@ -238,12 +260,12 @@ td_status trie_store_kv(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_
   if (r != TD_OK) return r;
   const td::DevState& s = c->dev;
   if ((r = bad_layers(c, layer_begin, n_layers)) != TD_OK) return r;
-  if (d_qslots ? q_max < 1 || q_max > (1 << 24) : q_max != s.b)
-    return fail(c, TD_EINVAL, "q_max must be in [1, 2^24], or the beam width for the leaves");
-  if ((int64_t)s.T * q_max >= (int64_t(1) << 31)) return fail(c, TD_EINVAL, "n_tries * q_max must be < 2^31");
+  if (d_qslots ? q_max < 1 : q_max != s.b) return fail(c, TD_EINVAL, "q_max must be >= 1, or the beam width for the leaves");
+  if ((int64_t)s.T * q_max > kStoreRows) return fail(c, TD_EINVAL, "n_tries * q_max must be at most 2^26");
   td::StoreArgs a{};
   if ((r = store_args(c, rope, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, &a)) != TD_OK) return r;
   if (d_qslots && c->pending) return fail(c, TD_ESTATE, "the leaves' K/V are pending: store them first");
+  if ((r = other_device(c)) != TD_OK) return r;
   a.rows = d_qslots ? td::PrefixRows::kNodes : td::PrefixRows::kLeaves;
   a.qslots = d_qslots;
   a.layer_begin = layer_begin;
@@ -272,39 +294,47 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
     return fail(c, TD_EINVAL, "positions [%d, +%d) outside the prefix's %d", pos, n, c->prefix_room);
   const int G = s.Hq / s.Hkv;
   if ((int64_t)n * G > (1 << 24)) return fail(c, TD_EINVAL, "n must be at most 2^24 / (Hq / Hkv)");
-  td::PrefixArgs a{};
-  a.q = d_q;
-  a.out = d_out;
-  a.rows = td::PrefixRows::kChunk;
-  a.layer_begin = layer_begin;
-  a.n_layers = n_layers;
-  a.tries = 1;
-  a.per_trie = a.q_stride = n;
-  a.pos0 = pos;
-  a.scale_log2 = scale * 1.4426950408889634f;
+  if (td_status r = other_device(c)) return r;
   const long rows = (long)n * G;
-  const int rpb = td::prefix_rows_per_block(s, rows);
-  a.row_blocks = (int)((rows + rpb - 1) / rpb);
-  const long keys = s.W > 0 ? std::min(pos + n, s.W) : pos + n;
-  const long fit = (long)(c->prefix_records / ((size_t)n_layers * n * s.Hq));
-  a.records = a.splits = td::prefix_splits(s, (long)n_layers * s.Hkv * a.row_blocks, keys, std::max(1l, fit));
-  a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
-  a.part_o = a.splits > 1 ? c->prefix_o : nullptr;
-  a.part_ml = c->prefix_ml;
+  const int rpb = td::prefix_rows_per_block(s, rows), blocks = (int)((rows + rpb - 1) / rpb);
+  // (as many layers per launch as its grid holds)
+  const int lc = (int)std::max(1l, std::min<long>(n_layers, (1l << 22) / ((long)s.Hkv * blocks)));
+  const size_t layer = (size_t)n * s.Hq * s.D * (s.dtype == TD_F32 ? 4 : 2);
   hipEvent_t ev0 = c->ev[TD_PHASE_ATTN][0], ev1 = c->ev[TD_PHASE_ATTN][1];
   c->ev[TD_PHASE_ATTN][0] = c->ev[TD_PHASE_ATTN][1] = nullptr;
-  hipError_t e = td::launch_prefix(s, a, st, ev0, a.part_o ? nullptr : ev1);
-  if (e == hipSuccess && a.part_o) {
-    td::PrefixMergeArgs m{};
-    m.prefix_o = c->prefix_o;
-  m.prefix_ml = c->prefix_ml;
-    m.prefix_splits = a.splits;
-    m.out = d_out;
-    m.rows = td::PrefixRows::kChunk;
-    m.n_layers = n_layers;
-    m.tries = 1;
-    m.per_trie = m.q_stride = n;
-    e = td::launch_prefix_merge(s, m, st, nullptr, ev1);
+  hipError_t e = hipSuccess;
+  for (int l = 0; l < n_layers && e == hipSuccess; l += lc) {
+    td::PrefixArgs a{};
+    a.q = static_cast<const char*>(d_q) + l * layer;
+    a.out = static_cast<char*>(d_out) + l * layer;
+    a.rows = td::PrefixRows::kChunk;
+    a.layer_begin = layer_begin + l;
+    a.n_layers = std::min(lc, n_layers - l);
+    a.tries = 1;
+    a.per_trie = a.q_stride = n;
+    a.pos0 = pos;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.row_blocks = blocks;
+    const long keys = s.W > 0 ? std::min(pos + n, s.W) : pos + n, units = (long)a.n_layers * s.Hkv * blocks;
+    const long fit = (long)(c->prefix_records / ((size_t)a.n_layers * n * s.Hq));
+    a.records = a.splits = td::prefix_splits(s, units, keys, std::max(1l, fit));
+    a.xcd_group = blocks > 1 && ((long)a.n_layers * s.Hkv * a.splits) % 8 == 0;
+    a.part_o = a.splits > 1 ? c->prefix_o : nullptr;
+    a.part_ml = c->prefix_ml;
+    hipEvent_t last = l + lc >= n_layers ? ev1 : nullptr;
+    e = td::launch_prefix(s, a, st, l == 0 ? ev0 : nullptr, a.part_o ? nullptr : last);
+    if (e == hipSuccess && a.part_o) {
+      td::PrefixMergeArgs m{};
+      m.prefix_o = c->prefix_o;
+      m.prefix_ml = c->prefix_ml;
+      m.prefix_splits = a.splits;
+      m.out = a.out;
+      m.rows = td::PrefixRows::kChunk;
+      m.n_layers = a.n_layers;
+      m.tries = 1;
+      m.per_trie = m.q_stride = n;
+      e = td::launch_prefix_merge(s, m, st, nullptr, last);
+    }
   }
   if (e != hipSuccess) return hip_fail(c, e, "trie_prefix_attn launch");
   return TD_OK;

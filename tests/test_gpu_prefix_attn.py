@@ -103,8 +103,9 @@ def test_decode_other_head_dims(dtype, D, T, b):
 
 
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 96)])
-def test_decode_vector_alu_kernel(dtype, D):
-    Batch(dtype, D, 4, 2, 100, 16, [(9, 3), (70, 2)], 4, attn_impl=B.TD_ATTN_VALU).decode()
+@pytest.mark.parametrize("S", [100, 2000])
+def test_decode_vector_alu_kernel(dtype, D, S):
+    Batch(dtype, D, 4, 2, S, 16, [(9, 3), (70, 2)], 4, attn_impl=B.TD_ATTN_VALU).decode()
 
 
 def test_splits_forced(monkeypatch):
@@ -323,6 +324,61 @@ def test_another_stream():
     bt.dec.attn_decode(0, 1, q, None, None, out, bt.scale, stream=side)
     side.synchronize()
     assert torch.equal(out, want)
+
+
+# where the tries' own nodes go: in the prefix's launch (short tries and prefixes), in a launch whose
+# epilogue merges the records (many units), in split launches and a merge; leaves stored by the call
+@pytest.mark.parametrize("D,Hq,Hkv,b,tries,S,L", [(128, 8, 2, 4, [(300, 6), (20, 2)], 1500, 1), (64, 16, 4, 16, [(200, 8)] * 12, 130, 4),
+                                                  (96, 8, 8, 3, [(1500, 4), (90, 2)], 40, 1), (128, 32, 8, 40, [(30, 3), (64, 1)], 700, 2)])
+@pytest.mark.parametrize("pending", [False, True])
+def test_where_the_nodes_go(D, Hq, Hkv, b, tries, S, L, pending):
+    bt = Batch("bf16", D, Hq, Hkv, S, 64, tries, b, L=L, dead=True)
+    if pending:  # the leaves' rows come with the call: the same rows, loaded as pending
+        k = torch.zeros((L, bt.T, b, Hkv, D), dtype=bt.dt, device="cuda")
+        v = torch.zeros_like(k)
+        for t, s in enumerate(bt.tries):
+            for j, n in enumerate(s["leaf_slot"]):
+                k[:, t, j], v[:, t, j] = bt.dec.k_pool[t, :, :, int(n)], bt.dec.v_pool[t, :, :, int(n)]
+        keep = bt.dec.k_pool.clone(), bt.dec.v_pool.clone()
+        for t, s in enumerate(bt.tries):
+            s["kv_pending"] = 1
+        bt.dec.close()
+        bt.dec = B.TrieDecoder(bt.T, b, keep[0].shape[3], 100, L, Hq, Hkv, D)
+        for t, s in enumerate(bt.tries):
+            bt.dec.load_state(t, s)
+        bt.dec.k_pool.copy_(keep[0])
+        bt.dec.v_pool.copy_(keep[1])
+        for t, s in enumerate(bt.tries):
+            for n in s["leaf_slot"]:
+                bt.dec.k_pool[t, :, :, int(n)] = bt.dec.v_pool[t, :, :, int(n)] = 7.0
+        bt.prefix.attach(bt.dec)
+        q = randn(bt.gen, (L, bt.T, b, Hq, D), bt.dt)
+        out = torch.empty_like(q)
+        bt.dec.attn_decode(0, L, q, k, v, out, bt.scale)
+        assert torch.equal(bt.dec.k_pool, keep[0]) and torch.equal(bt.dec.v_pool, keep[1])
+        again = torch.empty_like(q)
+        bt.dec.attn_decode(0, L, q, None, None, again, bt.scale)
+        assert float((again.float() - out.float()).abs().max()) <= 4 * 2.0 ** -8 * float(out.float().abs().max())
+    bt.decode(sample=0.05 if len(tries) > 2 else 0.3)
+
+
+def test_kernel_events():
+    """The attention's events bracket every launch of a call, beside a prefix too."""
+    bt = Batch("bf16", 128, 8, 2, 900, 64, [(150, 3), (90, 2)], 4, L=2)
+    q, out = randn(bt.gen, (2, 2, 4, 8, 128), bt.dt), torch.empty((2, 2, 4, 8, 128), dtype=bt.dt, device="cuda")
+    qs = torch.arange(90, dtype=torch.int32, device="cuda").repeat(2, 1)
+    tq = randn(bt.gen, (2, 2, 90, 8, 128), bt.dt)
+    cq = randn(bt.gen, (2, 50, 8, 128), bt.dt)
+    for call in (lambda: bt.dec.attn_decode(0, 2, q, None, None, out, bt.scale),
+                 lambda: bt.dec.tree_attn(0, 2, qs, tq, torch.empty_like(tq), bt.scale),
+                 lambda: bt.dec.tree_attn(0, 2, qs[:, -7:].contiguous(), tq[:, :, :7].contiguous(), torch.empty_like(tq[:, :, :7].contiguous()), bt.scale),
+                 lambda: bt.dec.prefix_attn(0, 2, 800, cq, torch.empty_like(cq), bt.scale)):
+        call()
+        ev = B.KernelEvents()
+        B.td_set_kernel_events(bt.dec.ctx, B.TD_PHASE_ATTN, ev.start, ev.stop)
+        call()
+        assert 0.0 < ev.elapsed_ms() < 50.0
+        ev.close()
 
 
 def test_refusals():
