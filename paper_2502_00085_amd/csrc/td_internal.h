@@ -127,6 +127,8 @@ struct AttnArgs {
                                    // grid's row_blocks counts WGs, of rb_per_wg blocks each
   int all_splits = 0;              // (matrix-core kernel) 1: every split WG takes a share of the
                                    // nodes (a forced split count); 0: only as many as needed
+  int half_wgs = 0;                // (matrix-core kernel) 1: 4-wave WGs, two per CU (two row blocks:
+                                   // no fused row copy, moves == 0)
   int partial = 0;                 // 1: partials, of one split too (a merge follows); 0: the output
   // records of the shared prefix (PrefixArgs::part_o, part_ml) to merge into the output; null: none
   const float* prefix_o = nullptr;
@@ -135,8 +137,6 @@ struct AttnArgs {
   int prefix_tries = 0;            // 1: those records hold the tries' own nodes too (no launch for them)
   // (prefill-shaped tree kernels beside a prefix) the launch's queries, q0 .. q0 + qn - 1 of each trie
   int q0 = 0, qn = 0;
-  int half_wgs = 0;                // (matrix-core kernel) 1: 4-wave WGs, two per CU (two row blocks:
-                                   // no fused row copy, moves == 0)
 };
 
 hipError_t launch_init_prompt(const DevState& s, const int32_t* h_plen, const int32_t* d_tokens,
