@@ -268,9 +268,10 @@ def _rows(t, dtype, shape, name):
     for n, st in reversed(rows):
         ok = ok and st == row
         row *= n
-    if not ok:
+    distance = rows[-1][1] if rows else heads * dim
+    if not ok or distance < heads * dim:  # (rows of an expanded tensor: distance 0)
         raise ValueError(f"{name}: rows must be contiguous and equally far apart, got strides {strides}")
-    return t.data_ptr(), rows[-1][1] if rows else heads * dim
+    return t.data_ptr(), distance
 
 
 def _store_rows(dims: Dims, lead, k, v, q, q_out):
@@ -287,6 +288,8 @@ def trie_prefix_store(ctx, dims: Dims, layer_begin: int, n_layers: int, pos: int
                       rope: Optional[Rope] = None, stream=None):
     """Store tokens pos, pos + 1, ... of the prefix: k / v [n_layers][n][Hkv][d] (k rotated), q
     [n_layers][n][Hq][d] rotated to q_out; their rows may be slices of a wider tensor's."""
+    if k is None and q is None:
+        raise ValueError("k and v, or q and q_out, must be given")
     n = int((q if k is None else k).shape[1])
     args = _store_rows(dims, (n_layers, n), k, v, q, q_out)
     _check(ctx, lib().trie_prefix_store(ctx, int(layer_begin), int(n_layers), int(pos), n,

@@ -229,6 +229,8 @@ def test_prefix_binding_checks_layouts_before_the_library():
     with pytest.raises(ValueError):
         B.trie_prefix_store(None, dims, 0, 2, 0, k, k)
     with pytest.raises(ValueError):
+        B.trie_prefix_store(None, dims, 0, 2, 0, None, None)
+    with pytest.raises(ValueError):
         B.Rope(torch.zeros(8))
 
 
@@ -262,7 +264,9 @@ def test_row_strides_of_a_fused_projection():
     assert rows(part.contiguous()) == (4096, 32)
     assert rows(part[:, :, :, :1]) == (4096, 336)
     assert B._rows(None, bf, (1,), "x") == (None, 0)
-    for bad in (part[:, :, :4], part.transpose(1, 2), part[..., :4], part[..., ::2, :]):
+    one = torch.zeros((1, 1, 1, 4, 8), dtype=bf)
+    for bad in (part[:, :, :4], part.transpose(1, 2), part[..., :4], part[..., ::2, :], one.expand(1, 1, 5, 4, 8),
+                one.expand(2, 3, 5, 4, 8), fused.as_strided((2, 3, 5, 4, 8), (240, 80, 16, 8, 1))):
         with pytest.raises(ValueError):
             rows(bad)
     with pytest.raises(ValueError):
