@@ -100,33 +100,27 @@ void note_written(td_ctx* c, int layer_begin, int n_layers) {
   if (all) c->pending = c->moves_pending = false;
 }
 
-// Ranges of layers whose moved rows are due.
-static std::vector<std::pair<int, int>> due_ranges(const td_ctx* c, int layer_begin, int n_layers) {
-  std::vector<std::pair<int, int>> due;
-  if (!c->pending || !c->moves_pending) return due;
-  for (int l = layer_begin; l < layer_begin + n_layers;) {
-    if (c->layer_written[l]) {
-      ++l;
-      continue;
-    }
-    int j = l;
-    while (j < layer_begin + n_layers && !c->layer_written[j]) ++j;
-    due.emplace_back(l, j - l);
-    l = j;
-  }
-  return due;
-}
+// Whether the rows that the last collection moved are still to be copied in layer l.
+static bool rows_due(const td_ctx* c, int l) { return c->pending && c->moves_pending && !c->layer_written[l]; }
 
 hipError_t copy_due_rows(td_ctx* c, int layer_begin, int n_layers, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
-  const auto due = due_ranges(c, layer_begin, n_layers);
+  const int end = layer_begin + n_layers;
+  auto next_due = [&](int l) {
+    while (l < end && !rows_due(c, l)) ++l;
+    return l;
+  };
   hipError_t e = hipSuccess;
-  for (size_t i = 0; i < due.size(); ++i)
-    if (e == hipSuccess)
-      e = launch_move_rows(c->dev, due[i].first, due[i].second, st, i == 0 ? ev0 : nullptr,
-                           i + 1 == due.size() ? ev1 : nullptr);
-  if (ev0 && due.empty()) {
-    if (e == hipSuccess) e = hipEventRecord(ev0, st);
+  int l = next_due(layer_begin);
+  if (ev0 && l == end) {
+    e = hipEventRecord(ev0, st);
     if (e == hipSuccess) e = hipEventRecord(ev1, st);
+  }
+  for (bool first = true; l < end && e == hipSuccess; first = false) {  // a launch per range of due layers
+    int j = l;
+    while (j < end && rows_due(c, j)) ++j;
+    const int n = j - l, next = next_due(j);
+    e = launch_move_rows(c->dev, l, n, st, first ? ev0 : nullptr, next == end ? ev1 : nullptr);
+    l = next;
   }
   return e;
 }
@@ -196,9 +190,9 @@ hipError_t attn_layers(td_ctx* c, int layer_begin, int n_layers, const void* d_q
   a.half_wgs = a.splits > 1 ? c->splits_override == 0 && sp.half_wgs
                             : mfma && a.row_blocks == 1 && attn_wgs > kOneRoundWgs;
   a.moves = 0;
-  const auto due = rows_copied ? std::vector<std::pair<int, int>>() : td::due_ranges(c, layer_begin, n_layers);
-  if (due.size() == 1 && due[0].second == n_layers && a.splits == 1 && a.row_blocks == 1 && !mv0 && fuse_moves)
-    a.moves = 1;
+  bool all_due = !rows_copied;
+  for (int l = layer_begin; l < layer_begin + n_layers; ++l) all_due = all_due && td::rows_due(c, l);
+  if (all_due && a.splits == 1 && a.row_blocks == 1 && !mv0 && fuse_moves) a.moves = 1;
   hipError_t e = hipSuccess;
   if (!a.moves && !rows_copied) e = td::copy_due_rows(c, layer_begin, n_layers, st, mv0, mv1);
   const bool prefix = c->prefix_length > 0;
@@ -499,8 +493,7 @@ td_status trie_tree_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32
     if (units * a.splits > ds.attn_pairs_max && a.splits > 1) a.splits = 1;
     a.half_wgs = a.splits > 1 && c->splits_override == 0 && sp.half_wgs;
     a.xcd_group = a.row_blocks > 1 && ((long)s.T * a.n_layers * s.Hkv * a.splits) % 8 == 0 ? 1 : 0;
-    a.partial = a.splits > 1 || prefix;
-      int prefix_splits = 0;
+    int prefix_splits = 0;
     bool tries = false;
     if (prefix)
       e = td::prefix_pass(c, true, a.layer_begin, a.n_layers, 0, q_max, q_max, d_qslots, a.q, a.scale_log2, 64, 0, st, first,
