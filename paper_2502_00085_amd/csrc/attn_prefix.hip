@@ -12,6 +12,19 @@
 // K in MFMA layout and V transposed (ds_read_b64_tr_b16) from a tile of 64 keys in LDS.  The tile's
 // rows come from the pages of a paged cache: a tile lies in one page of 64 keys or more, or in up to
 // four smaller ones, whose numbers are loaded a tile ahead by scalar loads.
+//
+// What bounds it, by the rows that share a key (times of one MI355X, d = 128 unless stated):
+//   * few rows: HBM.  8 rows per KV head (32 KV heads, d = 96) over 50,001 keys: 106 to 111 us, 5.5 to
+//     5.8 TB/s of reads.  Below some 4,000 keys per KV head a launch is a chain of latencies: 128 rows over 4,096
+//     keys of 8 KV heads, with the tries' own nodes, 17.7 us (its 17 MB take 3.4).
+//   * many rows: the SIMDs' issue.  1,024 rows of 8 KV heads over 8,192 keys of 4 layers: 151 to 167 us,
+//     828 to 911 TFLOP/s; the causal pass of 2,048 tokens from position 6,144: 249 to 267 us, 900 to 967 TFLOP/s (a
+//     library product of 8,192^3 makes 1,121 here).  There the matrix pipe is busy half of the CUs'
+//     clocks and the vector ALU (the exponentials) as long; LDS reads have no conflicts.  Each of the
+//     two waves of a SIMD fills the other's gaps.
+// Tried and not kept: four tile buffers (16,384 keys in 8 splits: 60 us against 48); 8 waves, of two
+// groups of keys, per 128 rows (8,192 keys, 1,024 rows: 55 us against 50); a fixed order of products and
+// LDS reads (1.5 % slower).
 #include <algorithm>
 
 #include "attn_common.h"
@@ -467,7 +480,8 @@ void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, h
 // Each (row, 8-element chunk of d) is merged by TP adjacent lanes, lane j taking the groups of 8
 // records j, j + TP, ...: every load of a group goes out before any is used; groups are merged with
 // a running shift, the lanes' states pairwise, in one order.  A record with sum 0 weighs nothing
-// (whatever its O); a NaN sum makes the row NaN.
+// (whatever its O); a NaN sum makes the row NaN.  Bound by the latency of its one or two loads in a
+// row: some 20 records each of 1,024 output rows, 4.5 to 5.3 us.
 constexpr int kMergeThreads = 64;
 
 template <typename T, int TP>
