@@ -11,13 +11,21 @@ constexpr float kPrefixNegBig = -1.0e30f;
 
 // (layer of the pass, KV head), row block and split of a WG.  The row blocks that read the same keys
 // lie 8 apart in the grid when xcd_group is set: on one XCD, whose L2 serves all but the first.  The
-// last block first: in a causal pass it has the longest range.
+// last block first: in a causal pass it has the longest range.  With pair_blocks an XCD takes the longer half
+// of its WGs longest first, then the shorter half shortest first, so that the two WGs of a CU make up
+// about the same length together.
 struct PrefixUnit {
   int li, g, rb, split;
 };
 __device__ inline PrefixUnit prefix_unit(const DevState& s, const PrefixArgs& a) {
   int x = blockIdx.x, rb;
-  if (a.xcd_group) {
+  if (a.xcd_group && a.pair_blocks) {
+    const int n = gridDim.x / 8, units = n / a.row_blocks, xcd = x % 8;
+    int k = x / 8;
+    if (k >= n / 2) k = n - 1 - (k - n / 2);
+    rb = k / units;
+    x = k % units * 8 + xcd;
+  } else if (a.xcd_group) {
     const int xcd = x % 8, k = x / 8;
     rb = k % a.row_blocks;
     x = (k / a.row_blocks) * 8 + xcd;

@@ -28,6 +28,7 @@ struct PrefixArgs {
   int row_blocks = 1, splits = 1;
   int records = 1;                  // per row: splits, and after them trie_splits
   int xcd_group = 0;                // row blocks of one (layer, KV head, split) on one XCD
+  int pair_blocks = 0;              // (with it, kChunk) an XCD's WGs in an order that evens out its CUs
   // (kLeaves, bf16) the same launch takes the tries' own nodes too, all of which are stored: after
   // prefix_wgs WGs come those of (layer, trie, KV head, block of a trie's rows, split of its nodes)
   int trie_splits = 0, trie_blocks = 0;

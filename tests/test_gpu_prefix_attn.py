@@ -220,6 +220,21 @@ def test_prefix_prefill_layers_and_splits():
     c.verify(c.run(), [0, 17, 39])
 
 
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,pos,n,window,L", [
+    ("bf16", 64, 16, 8, 0, 700, 0, 3),    # 264 blocks, an odd number per XCD, of 3 layers
+    ("bf16", 64, 16, 8, 5, 700, 100, 3),
+    ("bf16", 128, 32, 8, 90, 1024, 0, 2),  # 512
+    ("bf16", 96, 32, 32, 0, 1800, 0, 1),   # 480
+    ("f32", 64, 16, 8, 0, 1024, 0, 1)])    # 128 in 4 splits
+def test_prefix_prefill_two_blocks_per_cu(dtype, D, Hq, Hkv, pos, n, window, L):
+    """Launches whose blocks are ordered to even out the CUs: every block of every layer is taken."""
+    c = Chunk(dtype, D, Hq, Hkv, pos, n, 64, window, L)
+    out = c.run()
+    assert not (out == 5.0).all(-1).any()
+    step = 128 * Hkv // Hq
+    c.verify(out, range(step // 2, n, step))
+
+
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("bf16", 256), ("f32", 64), ("f32", 256)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("n,G", [(90, 4), (20, 1), (13, 4)])
