@@ -111,11 +111,12 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   if (trie_nodes > 0) {
     // the tries' own nodes in the same launch, where all of its WGs run at once, none has more than
     // kTrieTiles tiles of a trie, and the pass itself is short.  A step of 4 x 8 beams over 4,096 positions
-    // and 272 nodes each, a layer: 22.3 us, with a launch of its own for the tries 29.5; 2 x 4 beams over
-    // 50,001 positions (32 KV heads, 49 tiles per WG): 123.5 and 120.8.
+    // and 272 nodes each, a layer: 21.5 us, with a launch of its own for the tries 29.5; 2 x 4 beams over
+    // 50,001 positions (32 KV heads, 49 tiles per WG): 123.5 and 120.8.  A trie's WG has 3 of its tiles,
+    // which take about as long as the 4 that a WG of the prefix has at least (2: 22.3 us; 6: 25.7).
     const long wgs = (long)n_layers * s.Hkv * a.row_blocks * a.splits, tiles = (trie_nodes + 63) / 64;
     const long blocks = (qn * (s.Hq / s.Hkv) + rpb - 1) / rpb, units = (long)n_layers * s.T * s.Hkv * blocks;
-    const long ts = std::max(1l, std::min({(tiles + 1) / 2, 256 / units, fit - a.splits}));
+    const long ts = std::max(1l, std::min({(tiles + 2) / 3, 256 / units, fit - a.splits}));
     if (wgs + units * ts <= kOneRound && (keys + 63) / 64 <= (long)kShortPass * a.splits && (tiles + ts - 1) / ts <= kTrieTiles && a.splits + ts <= fit) {
       a.trie_splits = (int)ts;
       a.trie_blocks = (int)blocks;
