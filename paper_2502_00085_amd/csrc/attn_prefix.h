@@ -126,11 +126,29 @@ __device__ inline TilePages tile_pages(const PrefixHdr& h, int tile) {
 }
 
 // The keys [lo, hi) that some row of rows [r0, r0 + n) of a KV head sees, and [all_lo, all_hi) that all
-// of them see (those that see any), where they are known without asking the tries: causal rows
-// follow one another, and without a window every other row sees the whole prefix.
+// of them see (those that see any), where they are known without asking every row: causal rows
+// follow one another, without a window every other row sees the whole prefix, and the leaves of a trie
+// are of one depth (up to 8 tries in a block, whose headers come by scalar loads).
 __device__ inline bool prefix_range(const DevState& s, const PrefixArgs& a, const PrefixHdr& p, int r0, int n, PrefixSpan* w) {
   *w = {0, p.length, 0, p.length};
-  if (a.rows != PrefixRows::kChunk) return s.W <= 0;
+  if (a.rows != PrefixRows::kChunk && s.W <= 0) return true;
+  if (a.rows == PrefixRows::kNodes) return false;
+  if (a.rows == PrefixRows::kLeaves) {
+    const int per = a.per_trie * (s.Hq / s.Hkv), t0 = r0 / per, t1 = min((r0 + n - 1) / per, a.tries - 1);
+    if (t1 - t0 >= 8) return false;
+    int least = INT_MAX, most = INT_MIN;  // depths
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      typedef const __attribute__((address_space(4))) int32_t* cptr;
+      const int depth = *(cptr)(uintptr_t)&s.hdr[min(t0 + i, t1)].leaf_depth;
+      least = min(least, depth);
+      most = max(most, depth);
+    }
+    w->lo = max(0, p.length + least - s.W + 1);
+    w->all_lo = max(0, p.length + most - s.W + 1);
+    if (w->lo >= w->hi) *w = {0, 0, 0, 0};
+    return true;
+  }
   const int G = s.Hq / s.Hkv, first = a.pos0 + a.q0 + r0 / G, last = a.pos0 + a.q0 + min((r0 + n - 1) / G, a.per_trie - 1);
   w->hi = min(last + 1, p.room);
   w->all_hi = min(first + 1, p.room);
