@@ -16,9 +16,10 @@
 // What bounds it, by the rows that share a key (times of one MI355X, d = 128 unless stated):
 //   * few rows: HBM.  8 rows per KV head (32 KV heads, d = 96) over 50,001 keys: 106 to 111 us, 5.5 to
 //     5.8 TB/s of reads.  Below some 4,000 keys per KV head a launch is a chain of latencies: 128 rows over 4,096
-//     keys of 8 KV heads, with the tries' own nodes, 17.7 us (its 17 MB take 3.4).
+//     keys of 8 KV heads, with the tries' own nodes, 17.0 us (its 17 MB take 3.4).
 //   * many rows: the clock under matrix load.  1,024 rows of 8 KV heads over 8,192 keys of 4 layers: 151 to 167 us,
-//     828 to 911 TFLOP/s; the causal pass of 2,048 tokens from position 6,144: 240 us, 1,002 TFLOP/s (a
+//     828 to 911 TFLOP/s; the causal pass of 2,048 tokens from position 6,144: 240 to
+//     245 us, 983 to 1,002 TFLOP/s (a
 //     library product of 8,192^3 makes 1,121 here).  There the card runs at 1.9 of its 2.4 GHz, the
 //     matrix pipe busy for half of the clocks, the vector ALU (the exponentials) as long, LDS a quarter.
 //     Each of the two waves of a SIMD fills the other's gaps: a loop that interleaves one half's weights
@@ -482,7 +483,7 @@ void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, h
 // records j, j + TP, ...: every load of a group goes out before any is used; groups are merged with
 // a running shift, the lanes' states pairwise, in one order.  A record with sum 0 weighs nothing
 // (whatever its O); a NaN sum makes the row NaN.  Bound by the latency of its one or two loads in a
-// row: some 20 records each of 1,024 output rows, 4.5 to 5.3 us.
+// row: 18 records each of 1,024 output rows, 4.7 to 5.1 us.
 constexpr int kMergeThreads = 64;
 
 template <typename T, int TP>
