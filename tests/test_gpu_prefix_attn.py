@@ -120,6 +120,15 @@ def test_decode_window(dtype, D, window):
     Batch(dtype, D, 8, 2, 130, 16, [(3, 2), (33, 1), (90, 4), (1, 0)], 4, window=window, dead=True).decode()
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 64), ("bf16", 32)])
+def test_decode_window_tries_of_other_depths(dtype, D):
+    """Tries of one row block at other depths: the window leaves some of them nothing of the prefix, others a
+    part; few tries and more than a block takes the headers of."""
+    Batch(dtype, D, 4, 2, 100, 16, [(5, 2), (60, 2), (1, 1), (200, 1)], 3, window=64).decode()
+    Batch(dtype, D, 4, 2, 300, 32, [(1 + 13 * i, 1 + i % 3) for i in range(13)], 2, window=90).decode()
+    Batch(dtype, D, 4, 2, 40, 16, [(90, 2), (80, 1)], 3, window=64).decode()  # (nothing for any)
+
+
 def test_one_live_leaf_and_many_layers():
     bt = Batch("bf16", 128, 8, 2, 300, 64, [(12, 0), (40, 3)], 6, L=5)
     q, out = bt.decode(sample=0.3)
