@@ -119,7 +119,8 @@ typedef struct {
   int32_t base;         /* physical slot of logical slot 0 (read only)                    */
   int32_t n_shared;     /* leading slots on every live beam's path (read only)            */
   int32_t next_id;      /* id of the next appended node (prompt P, then P + s*b)          */
-  int32_t kv_pending;   /* 1: the leaves' K/V rows are not yet in the pools; the next     */
+  int32_t kv_pending;   /* 1: the leaves' K/V rows are not yet in the pools (of every     */
+                        /*    layer); trie_store_kv stores them, or the next              */
                         /*    trie_attn_decode call(s) must pass k_new/v_new              */
   int32_t step;         /* appends so far (decode steps taken since the prompt)           */
   int32_t* node_id;     /* [N] prompt token j -> j; step s rank j -> P + (s-1)*b + j     */
@@ -158,8 +159,10 @@ td_status td_init_prompt(td_ctx* ctx, const int32_t* h_prompt_len, const int32_t
  * reads KV head h / (Hq/Hkv).  When the leaves' K/V are pending (after an append), the
  * call first copies the rows the append's compaction moved (layers not done yet), then
  * stores k_new/v_new into the leaves' pool rows, and the leaves attend to them;
- * otherwise (or after trie_store_kv of every layer of the call) d_k_new/d_v_new must be NULL.  fp32 accumulation; out rows of beams
- * >= n_live are zeroed.  scale is normally 1/sqrt(d). */
+ * otherwise, and after trie_store_kv of every layer of the call, d_k_new/d_v_new must be NULL
+ * (else TD_EINVAL).  A call over some layers that trie_store_kv has stored and some that are
+ * still due needs them, and stores them for all of its layers: they replace trie_store_kv's
+ * rows.  fp32 accumulation; out rows of beams >= n_live are zeroed.  scale is normally 1/sqrt(d). */
 td_status trie_attn_decode(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, const void* d_q,
                            const void* d_k_new, const void* d_v_new, void* d_out, float scale,
                            hipStream_t stream);
@@ -245,7 +248,8 @@ td_status trie_prefix_attn(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, i
  *   d_qslots NULL: the live leaves in rank order, q_max = b; rows of beams >= n_live store nothing,
  *   and their q_out is zero.  With K/V this is the store that trie_attn_decode does from k_new /
  *   v_new (rows moved by a collection are copied first): the layers' rows are no longer pending, and
- *   trie_attn_decode of these layers takes NULL k_new / v_new. */
+ *   trie_attn_decode of these layers takes NULL k_new / v_new (see there for a call that has other
+ *   layers too). */
 td_status trie_store_kv(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t q_max, const int32_t* d_qslots,
                         const td_rope* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
                         const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t stream);
@@ -309,11 +313,10 @@ td_status beam_logsoftmax_topk(td_ctx* ctx, const float* d_logits, int32_t* d_se
  * parent died).  If the room after the compacted trie is smaller than the (g-1)*b slots
  * the appends before the next collection need, the trie is re-packed at slot 0.  The
  * K/V rows of moved survivors are copied to their new slots by the next trie_attn_decode
- * call of each layer, before it reads them (until then the pools hold those rows at their
- * old slots; td_init_prompt drops every copy still due, td_load_state those of the trie it
- * loads).  The new leaves
- * become the last b slots in rank j order; their K/V rows are pending until the next
- * trie_attn_decode.
+ * (or trie_store_kv of the leaves) call of each layer, before it reads or stores rows (until
+ * then the pools hold those rows at their old slots; td_init_prompt drops every copy still
+ * due, td_load_state those of the trie it loads).  The new leaves become the last b slots in
+ * rank j order; their K/V rows are pending until the next trie_attn_decode or trie_store_kv.
  * Inputs [T][b] device.  Invalid selections / capacity overflow (a trie without room for
  * its next b nodes after any collection of this call): sticky device status, trie
  * unchanged. */
@@ -373,8 +376,8 @@ td_status td_read_state(td_ctx* ctx, int32_t trie, td_state* host_out);
 /* Replace trie t by a host state (synchronous).  Slots are placed at base 0, and row
  * copies still due for trie t are dropped; those of the other tries stay due.  With other
  * initialised tries, kv_pending must equal theirs (else TD_EINVAL), and a state with
- * kv_pending = 1 is accepted only before the step's first trie_attn_decode (else
- * TD_ESTATE): the next attention calls then store its leaves' rows too.  The state
+ * kv_pending = 1 is accepted only before the step's first trie_attn_decode or trie_store_kv
+ * of the leaves (else TD_ESTATE): those calls then store its leaves' rows too.  The state
  * must be one the method can produce: depth non-decreasing along slots, parents before
  * children with depth + 1, leaves = last n_live slots in rank order with one-hot masks,
  * no all-beam slot after a slot on only some paths (dead slots, mask 0, may lie anywhere

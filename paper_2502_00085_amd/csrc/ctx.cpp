@@ -92,9 +92,9 @@ td_status check_ready(td_ctx* c) {
   return TD_OK;
 }
 
-void note_written(td_ctx* c, int layer_begin, int n_layers) {
+void note_written(td_ctx* c, int layer_begin, int n_layers, LayerRows by) {
   if (!c->pending) return;
-  for (int l = layer_begin; l < layer_begin + n_layers; ++l) c->layer_written[l] = 1;
+  for (int l = layer_begin; l < layer_begin + n_layers; ++l) c->layer_written[l] = (uint8_t)by;
   bool all = true;
   for (int l = 0; l < c->dev.L; ++l) all = all && c->layer_written[l];
   if (all) c->pending = c->moves_pending = false;
@@ -377,12 +377,17 @@ td_status trie_attn_decode(td_ctx* c, int32_t layer_begin, int32_t n_layers, con
     return fail(c, TD_EINVAL, "layer range [%d, %d) outside [0, %d)", layer_begin, layer_begin + n_layers, s.L);
   if (!d_q || !d_out || !aligned16(d_q) || !aligned16(d_out))
     return fail(c, TD_EINVAL, "q / out must be non-null and 16-byte aligned");
-  bool stored = true;  // (by trie_store_kv, for every layer of the call)
-  for (int l = layer_begin; l < layer_begin + n_layers; ++l) stored = stored && (!c->pending || c->layer_written[l]);
+  bool stored = true, apart = true;  // every layer of the call: stored; by trie_store_kv
+  for (int l = layer_begin; l < layer_begin + n_layers; ++l) {
+    stored = stored && (!c->pending || c->layer_written[l]);
+    apart = apart && c->layer_written[l] == (uint8_t)td::LayerRows::kStored;
+  }
   if (!stored && (!d_k_new || !d_v_new))
     return fail(c, TD_EINVAL, "the leaves' K/V are pending: k_new and v_new are required");
   if (!c->pending && (d_k_new || d_v_new))
     return fail(c, TD_EINVAL, "no leaf K/V is pending (after init/load): pass NULL k_new / v_new");
+  if (c->pending && apart && (d_k_new || d_v_new))
+    return fail(c, TD_EINVAL, "trie_store_kv has stored the leaves' K/V of these layers: pass NULL k_new / v_new");
   if ((d_k_new == nullptr) != (d_v_new == nullptr)) return fail(c, TD_EINVAL, "pass both k_new and v_new, or neither");
   if (c->pending && (!aligned16(d_k_new) || !aligned16(d_v_new)))
     return fail(c, TD_EINVAL, "k_new / v_new must be 16-byte aligned");
@@ -405,7 +410,7 @@ td_status trie_attn_decode(td_ctx* c, int32_t layer_begin, int32_t n_layers, con
                     l == 0 ? ev0 : nullptr, l + n == n_layers ? ev1 : nullptr, mv0, mv1);
   }
   if (e != hipSuccess) return hip_fail(c, e, "trie_attn_decode launch");
-  td::note_written(c, layer_begin, n_layers);
+  if (d_k_new) td::note_written(c, layer_begin, n_layers, td::LayerRows::kAttended);
   return TD_OK;
 }
 

@@ -14,7 +14,7 @@ struct td_ctx {
   int device = 0;
   std::vector<uint8_t> inited;         // per trie: initialised by init_prompt / load_state
   bool pending = false;                // leaves' K/V rows not yet stored in the pools
-  std::vector<uint8_t> layer_written;  // per layer, while pending
+  std::vector<uint8_t> layer_written;  // per layer, while pending: LayerRows
   bool moves_pending = false;          // rows moved by the last compaction not yet copied
                                        //   (for the layers not yet written)
   std::vector<int32_t> leaf_depth;     // per trie: depth of its live leaves (mirrors the
@@ -44,8 +44,11 @@ td_status hip_fail(td_ctx* c, hipError_t e, const char* what);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 // TD_ESTATE unless every trie is initialised.
 td_status check_ready(td_ctx* c);
+// Whether a layer's leaf rows are in the pools, and from which call: the attention's k_new / v_new, which
+// may come again with the next call, or trie_store_kv, whose rotated rows they must not replace.
+enum class LayerRows : uint8_t { kDue = 0, kAttended = 1, kStored = 2 };
 // Marks the leaves' rows of layers [layer_begin, +n_layers) as stored.
-void note_written(td_ctx* c, int layer_begin, int n_layers);
+void note_written(td_ctx* c, int layer_begin, int n_layers, LayerRows by);
 // Copies the rows the last collection moved, for the layers of the range that are still due (ev0, ev1:
 // the copy's events, both or neither).
 hipError_t copy_due_rows(td_ctx* c, int layer_begin, int n_layers, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1);

@@ -277,7 +277,7 @@ td_status trie_store_kv(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_
   hipError_t e = a.k ? td::copy_due_rows(c, layer_begin, n_layers, st, nullptr, nullptr) : hipSuccess;
   if (e == hipSuccess) e = td::launch_store(s, a, st);
   if (e != hipSuccess) return hip_fail(c, e, "trie_store_kv launch");
-  if (a.k) td::note_written(c, layer_begin, n_layers);
+  if (a.k) td::note_written(c, layer_begin, n_layers, td::LayerRows::kStored);
   return TD_OK;
 }
 

@@ -212,3 +212,45 @@ def test_store_call_order():
     dec.append_prune(sel[0], sel[1], sel[2])
     assert dec.status() == 0
     dec.close()
+
+
+def test_rows_given_again_for_stored_layers():
+    """k_new / v_new of layers whose rows store_kv has stored (rotated) are refused while other layers are
+    pending too: nothing is overwritten.  Layers that the attention stored take them again, as ever."""
+    gen, dt, L = torch.Generator().manual_seed(8), torch.bfloat16, 3
+    dec = B.TrieDecoder(1, 2, 60, 50, L, 2, 1, 64)
+    dec.init_prompt([20], torch.zeros((1, 20), dtype=torch.int32, device="cuda"))
+    rope = B.Rope(freqs(64))
+    q, k, v = (randn(gen, (L, 1, 2, h, 64), dt) for h in (2, 1, 1))
+    out = torch.zeros_like(q)
+    sel = [torch.zeros((1, 2), dtype=x, device="cuda") for x in (torch.int32, torch.int32, torch.float32, torch.float32)]
+
+    def refused(l, n):
+        pools = dec.k_pool.clone(), dec.v_pool.clone()
+        with pytest.raises(B.TdError) as e:
+            dec.attn_decode(l, n, q[l:l + n], k[l:l + n], v[l:l + n], out[l:l + n], 0.1)
+        assert e.value.status == B.TD_EINVAL
+        assert torch.equal(pools[0], dec.k_pool) and torch.equal(pools[1], dec.v_pool)
+
+    dec.attn_decode(0, L, q, None, None, out, 0.1)
+    for step in range(2):
+        dec.topk_append(torch.randn((1, 2, 50), generator=gen).cuda(), *sel)
+        dec.store_kv(0, 2, k[:2], v[:2], rope=rope)
+        for l, n in ((0, 1), (1, 1), (0, 2)):
+            refused(l, n)
+        dec.attn_decode(0, 2, q[:2], None, None, out[:2], 0.1)
+        refused(0, 1)  # (read by the attention, and still store_kv's)
+        if step == 0:
+            dec.attn_decode(2, 1, q[2], k[2], v[2], out[2], 0.1)
+        else:
+            dec.store_kv(2, 1, k[2:], v[2:], rope=rope)
+        refused(2, 1)  # (nothing is pending any more)
+        refused(0, L)
+    dec.topk_append(torch.randn((1, 2, 50), generator=gen).cuda(), *sel)
+    for _ in range(2):
+        dec.attn_decode(0, 1, q[0], k[0], v[0], out[0], 0.1)
+    dec.store_kv(0, 1, k[:1], v[:1], rope=rope)
+    refused(0, 1)
+    dec.attn_decode(1, 2, q[1:], k[1:], v[1:], out[1:], 0.1)
+    assert dec.status() == 0
+    dec.close()
