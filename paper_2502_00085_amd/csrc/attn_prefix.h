@@ -160,22 +160,22 @@ __device__ inline bool prefix_range(const DevState& s, const PrefixArgs& a, cons
   return true;
 }
 
-// The same from the rows of RW waves (rw < RW; every thread calls it).
+// The same from the rows of RW waves (rw < RW; every thread calls it; red: 4 RW words).
 template <int RW>
-__device__ inline PrefixSpan prefix_range_of(const PrefixSpan& w, int rw, bool writes, int (*red)[RW]) {
+__device__ inline PrefixSpan prefix_range_of(const PrefixSpan& w, int rw, bool writes, int* red) {
   if (writes) {
-    red[0][rw] = w.lo;
-    red[1][rw] = w.hi;
-    red[2][rw] = w.all_lo;
-    red[3][rw] = w.all_hi;
+    red[rw] = w.lo;
+    red[RW + rw] = w.hi;
+    red[2 * RW + rw] = w.all_lo;
+    red[3 * RW + rw] = w.all_hi;
   }
   __syncthreads();
   PrefixSpan r = {INT_MAX, 0, 0, INT_MAX};
   for (int i = 0; i < RW; ++i) {
-    r.lo = min(r.lo, red[0][i]);
-    r.hi = max(r.hi, red[1][i]);
-    r.all_lo = max(r.all_lo, red[2][i]);
-    r.all_hi = min(r.all_hi, red[3][i]);
+    r.lo = min(r.lo, red[i]);
+    r.hi = max(r.hi, red[RW + i]);
+    r.all_lo = max(r.all_lo, red[2 * RW + i]);
+    r.all_hi = min(r.all_hi, red[3 * RW + i]);
   }
   r.lo = __builtin_amdgcn_readfirstlane(r.lo);
   r.hi = __builtin_amdgcn_readfirstlane(r.hi);

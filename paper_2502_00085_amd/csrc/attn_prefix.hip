@@ -64,13 +64,13 @@ template <int D, int RW, int KW, bool TRIES>
 __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k_attn_prefix(DevState s, PrefixArgs a) {
   using C = PrefixCfg<D, RW, KW>;
   static_assert(2 * C::LOADS < 64, "the wait counter holds a tile's loads");
-  static_assert(KW == 1 || KW == 2, "one or two groups");
+  static_assert(KW == 1 || KW == 2, "one or two groups: the RW KW waves have a word each of wred");
   constexpr int NH = 2 / KW;  // 32-key halves of a tile per wave
   // (an array per buffer: the compiler can tell an operand read of one buffer from the direct loads
   // under way into the others)
   __shared__ __attribute__((aligned(16))) unsigned char kbuf0[2 * C::HALF], vbuf0[2 * C::HALF];
   __shared__ __attribute__((aligned(16))) unsigned char kbuf1[2 * C::HALF], vbuf1[2 * C::HALF];
-  __shared__ int wred[4][RW];
+  __shared__ int wred[4 * RW];
   __shared__ float ml[KW == 2 ? RW * 128 : 1];
   PrefixHdr p = *s.prefix;
   const bool trie = TRIES && blockIdx.x >= a.prefix_wgs;
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   PrefixSpan span, all;  // (of the wave; of the WG)
   bool known = true;
   if (TRIES && trie) {
-    const int lo = window_lo(s, t, th.base, th.n_nodes, th.leaf_depth, wred[0]);
+    const int lo = window_lo(s, t, th.base, th.n_nodes, th.leaf_depth, wred);  // (a word per wave)
     __syncthreads();
     const int shared = max(lo, min(th.n_shared, th.n_nodes));
     all = {lo, th.n_nodes, lo, shared};

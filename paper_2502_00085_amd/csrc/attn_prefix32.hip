@@ -47,7 +47,7 @@ template <int D, int RW, int KW>
 __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void k_attn_prefix32(DevState s, PrefixArgs a) {
   using C = Prefix32Cfg<D, RW, KW>;
   __shared__ __attribute__((aligned(16))) unsigned char kbuf[C::TILE], vbuf[C::TILE];
-  __shared__ int wred[4][RW];
+  __shared__ int wred[4 * RW];
   __shared__ float ml[KW == 2 ? RW * 128 : 1];
   const PrefixHdr p = *s.prefix;
   const PrefixUnit u = prefix_unit(s, a);
