@@ -104,7 +104,12 @@ struct MfmaCfg {
 // part: about 6.6 against 6.1 TB/s for a 279 MB span read cold by 256 WGs).  Off where
 // sibling WGs of other row blocks read the same range again from L2 (xcd_group) and for
 // the tree kernel, whose row blocks share the keys the same way.
-template <int D, int NW, bool TREE, int RB, bool NT>
+//
+// PFX: an unsplit launch that merges the records of a shared prefix into its output (AttnArgs::prefix_o).
+// An instance of its own: the merge in the epilogue of every instance, behind a test of the pointer, cost
+// the calls without a prefix 0.5 to 1 % (graphs of one-layer calls, replayed in turn: 8 beams over 2,112
+// nodes, 32 layers, 409.3 -> 411.6 us; 2 beams over 23, 16 layers, 124.2 -> 125.4).
+template <int D, int NW, bool TREE, int RB, bool NT, bool PFX>
 __global__ __launch_bounds__(NW * 64, 2) void k_attn_mfma(DevState s, AttnArgs a) {
   static_assert(RB == 1 || (RB == 2 && !TREE), "two row blocks per WG: decode only");
   static_assert(NW == 8 || NW == 4, "WGs of 4 or 8 waves");
@@ -678,13 +683,13 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_mfma(DevState s, AttnArgs a
         O[4] += x1.x * f; O[5] += x1.y * f; O[6] += x1.z * f; O[7] += x1.w * f;
       }
       float Mi = rowm[i], L = rowl[i];
-      if (!a.partial) {
+      if (PFX || !a.partial) {
         const int rr = (u.rb * RB + rbk) * kRows + i;
         if (rr < nrows * G) {
           const int bm = rr / G;
           const size_t row = (((size_t)u.li * s.T + u.t) * nrows + bm) * s.Hq + u.g * G + rr % G;
           bool live = (TREE || bm < n_live) && L > 0.0f;
-          if (a.prefix_o != nullptr) {
+          if constexpr (PFX) {
             merge_prefix(s, a, row, c, Mi, L, O);
             live = (TREE || bm < n_live) && L != 0.0f;  // (a NaN sum: a NaN row)
           }
@@ -722,6 +727,18 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_mfma(DevState s, AttnArgs a
 
 constexpr int kNW = 8;
 constexpr int kCUs = 256;
+
+template <int D, int NW, bool TREE, int RB, bool NT>
+void launch_one(const DevState& s, const AttnArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
+  const dim3 grid(s.T * a.n_layers * s.Hkv * a.row_blocks * a.splits), block(NW * 64);
+  if constexpr (NW == kNW || NT) {
+    if (a.prefix_o) {
+      hipExtLaunchKernelGGL((k_attn_mfma<D, NW, TREE, RB, NT, true>), grid, block, 0, st, ev0, ev1, 0, s, a);
+      return;
+    }
+  }
+  hipExtLaunchKernelGGL((k_attn_mfma<D, NW, TREE, RB, NT, false>), grid, block, 0, st, ev0, ev1, 0, s, a);
+}
 
 }  // namespace
 
@@ -781,22 +798,18 @@ hipError_t launch_attn_mfma(const DevState& s, const AttnArgs& a, hipStream_t st
       a.row_blocks32 > a.row_blocks * a.rb_per_wg || a.row_blocks32 <= (a.row_blocks - 1) * a.rb_per_wg)
     return hipErrorInvalidValue;
   if (a.half_wgs && a.rb_per_wg == 2 && a.moves) return hipErrorInvalidValue;
-  const dim3 grid(s.T * a.n_layers * s.Hkv * a.row_blocks * a.splits), block(kNW * 64), half(kNW * 32);
-#define LAUNCH_MFMA(DD)                                                                                      \
-  (a.tree && a.half_wgs                                                                                        \
-       ? hipExtLaunchKernelGGL((k_attn_mfma<DD, kNW / 2, true, 1, false>), grid, half, 0, st, ev0, ev1, 0, s, a) \
-   : a.tree ? hipExtLaunchKernelGGL((k_attn_mfma<DD, kNW, true, 1, false>), grid, block, 0, st, ev0, ev1, 0, s, a) \
-   : a.half_wgs && a.rb_per_wg == 2                                                                            \
-       ? hipExtLaunchKernelGGL((k_attn_mfma<DD, kNW / 2, false, 2, true>), grid, half, 0, st, ev0, ev1, 0, s, a) \
-   : a.half_wgs && a.xcd_group                                                                                 \
-       ? hipExtLaunchKernelGGL((k_attn_mfma<DD, kNW / 2, false, 1, false>), grid, half, 0, st, ev0, ev1, 0, s, a) \
-   : a.half_wgs                                                                                                \
-       ? hipExtLaunchKernelGGL((k_attn_mfma<DD, kNW / 2, false, 1, true>), grid, half, 0, st, ev0, ev1, 0, s, a) \
-   : a.rb_per_wg == 2                                                                                          \
-       ? hipExtLaunchKernelGGL((k_attn_mfma<DD, kNW, false, 2, true>), grid, block, 0, st, ev0, ev1, 0, s, a)  \
-   : a.xcd_group                                                                                               \
-       ? hipExtLaunchKernelGGL((k_attn_mfma<DD, kNW, false, 1, false>), grid, block, 0, st, ev0, ev1, 0, s, a) \
-       : hipExtLaunchKernelGGL((k_attn_mfma<DD, kNW, false, 1, true>), grid, block, 0, st, ev0, ev1, 0, s, a))
+  // (records of a prefix are merged by unsplit launches, whose half-size WGs are those of decode calls of
+  // one WG per unit)
+  if (a.prefix_o && (a.splits > 1 || a.partial || (a.half_wgs && (a.tree || a.xcd_group)))) return hipErrorInvalidValue;
+#define LAUNCH_MFMA(DD)                                                                   \
+  (a.tree && a.half_wgs             ? launch_one<DD, kNW / 2, true, 1, false>(s, a, st, ev0, ev1) \
+   : a.tree                         ? launch_one<DD, kNW, true, 1, false>(s, a, st, ev0, ev1)     \
+   : a.half_wgs && a.rb_per_wg == 2 ? launch_one<DD, kNW / 2, false, 2, true>(s, a, st, ev0, ev1) \
+   : a.half_wgs && a.xcd_group      ? launch_one<DD, kNW / 2, false, 1, false>(s, a, st, ev0, ev1) \
+   : a.half_wgs                     ? launch_one<DD, kNW / 2, false, 1, true>(s, a, st, ev0, ev1) \
+   : a.rb_per_wg == 2               ? launch_one<DD, kNW, false, 2, true>(s, a, st, ev0, ev1)     \
+   : a.xcd_group                    ? launch_one<DD, kNW, false, 1, false>(s, a, st, ev0, ev1)    \
+                                    : launch_one<DD, kNW, false, 1, true>(s, a, st, ev0, ev1))
   switch (s.D) {
     case 64: LAUNCH_MFMA(64); break;
     case 96: LAUNCH_MFMA(96); break;

@@ -92,7 +92,8 @@ __device__ inline void load_words(const uint32_t* p, uint32_t* w) {
   }
 }
 
-template <typename T, int D, int RT>
+// PFX: an unsplit launch that merges the records of a shared prefix into its output (AttnArgs::prefix_o).
+template <typename T, int D, int RT, bool PFX>
 __global__ __launch_bounds__((Cfg32<T, D, RT>::NW * 64), (Cfg32<T, D, RT>::NW / 4)) void k_attn_mfma32(DevState s, AttnArgs a) {
   using C = Cfg32<T, D, RT>;
   constexpr int NW = C::NW;
@@ -413,13 +414,13 @@ __global__ __launch_bounds__((Cfg32<T, D, RT>::NW * 64), (Cfg32<T, D, RT>::NW / 
       O += *reinterpret_cast<const f32x4*>(obuf + (w * C::ROWS + i) * C::OS + c) * f;
     }
     float L = rowl[i];
-    if (!a.partial) {
+    if (PFX || !a.partial) {
       const int r = u.rb * C::ROWS + i;
       if (r < s.b * G) {
         const int bm = r / G;
         const size_t row = (((size_t)u.li * s.T + u.t) * s.b + bm) * s.Hq + u.g * G + r % G;
         bool live = bm < n_live && L > 0.0f;
-        if (a.prefix_o != nullptr) {
+        if constexpr (PFX) {
           float M = rowm[i], o4[4] = {O[0], O[1], O[2], O[3]};
           merge_prefix(s, a, row, c, M, L, o4);
           O = f32x4{o4[0], o4[1], o4[2], o4[3]};
@@ -447,10 +448,14 @@ __global__ __launch_bounds__((Cfg32<T, D, RT>::NW * 64), (Cfg32<T, D, RT>::NW / 
 template <typename T, int RT>
 hipError_t launch_rt(const DevState& s, const AttnArgs& a, dim3 grid, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
   switch (s.D) {
-#define MFMA32_CASE(DD)                                                                                        \
-    case DD:                                                                                                   \
-      hipExtLaunchKernelGGL((k_attn_mfma32<T, DD, RT>), grid, dim3(Cfg32<T, DD, RT>::NW * 64), 0, st, ev0, ev1, 0, \
-                            s, a);                                                                              \
+#define MFMA32_CASE(DD)                                                                                            \
+    case DD:                                                                                                       \
+      if (a.prefix_o)                                                                                              \
+        hipExtLaunchKernelGGL((k_attn_mfma32<T, DD, RT, true>), grid, dim3(Cfg32<T, DD, RT>::NW * 64), 0, st, ev0, \
+                              ev1, 0, s, a);                                                                       \
+      else                                                                                                         \
+        hipExtLaunchKernelGGL((k_attn_mfma32<T, DD, RT, false>), grid, dim3(Cfg32<T, DD, RT>::NW * 64), 0, st, ev0, \
+                              ev1, 0, s, a);                                                                       \
       break;
     MFMA32_CASE(32) MFMA32_CASE(160) MFMA32_CASE(192) MFMA32_CASE(224) MFMA32_CASE(256)
     case 64: case 96: case 128:
@@ -527,6 +532,7 @@ AttnKernel attn_kernel(const DevState& s, int attn_impl, int n_layers, long max_
 
 hipError_t launch_attn_mfma32(const DevState& s, const AttnArgs& a, hipStream_t st, hipEvent_t ev0,
                               hipEvent_t ev1) {
+  if (a.prefix_o && (a.splits > 1 || a.partial)) return hipErrorInvalidValue;
   const dim3 grid(s.T * a.n_layers * s.Hkv * a.row_blocks * a.splits);
   const bool one = attn_mfma32_rows_per_block(s) == 16;
   if (s.dtype == TD_F32)

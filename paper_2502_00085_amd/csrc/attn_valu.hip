@@ -42,7 +42,8 @@ __device__ inline void merge_state(float& m, float& l, float m2, float l2, float
   m = M;
 }
 
-template <typename T, int EPL>
+// PFX: an unsplit launch that merges the records of a shared prefix into its output (AttnArgs::prefix_o).
+template <typename T, int EPL, bool PFX>
 __global__ __launch_bounds__(kValuThreads) void k_attn_valu(DevState s, AttnArgs a) {
   constexpr int DD = 16 * EPL;
   constexpr int R = valu_rows(DD);
@@ -176,13 +177,13 @@ __global__ __launch_bounds__(kValuThreads) void k_attn_valu(DevState s, AttnArgs
       L += sl[w][i] * f;
       O += so[w][i][c] * f;
     }
-    if (!a.partial) {
+    if (PFX || !a.partial) {
       const int r = u.rb * R + i;
       if (r < s.b * G) {
         const int bm = r / G, hl = r % G;
         const size_t row = (((size_t)u.li * s.T + u.t) * s.b + bm) * s.Hq + u.g * G + hl;
         bool live = bm < n_live && L > 0.0f;
-        if (a.prefix_o != nullptr) {
+        if constexpr (PFX) {
           float o1[1] = {O};
           merge_prefix(s, a, row, c, M, L, o1);
           O = o1[0];
@@ -207,8 +208,11 @@ hipError_t launch_t(const DevState& s, const AttnArgs& a, dim3 grid, hipStream_t
                     hipEvent_t ev1) {
   const dim3 block(kValuThreads);
   switch (s.D) {
-#define VALU_CASE(DD) \
-    case DD: hipExtLaunchKernelGGL((k_attn_valu<T, DD / 16>), grid, block, 0, st, ev0, ev1, 0, s, a); break;
+#define VALU_CASE(DD)                                                                                                \
+    case DD:                                                                                                         \
+      if (a.prefix_o) hipExtLaunchKernelGGL((k_attn_valu<T, DD / 16, true>), grid, block, 0, st, ev0, ev1, 0, s, a); \
+      else hipExtLaunchKernelGGL((k_attn_valu<T, DD / 16, false>), grid, block, 0, st, ev0, ev1, 0, s, a);           \
+      break;
     VALU_CASE(32) VALU_CASE(64) VALU_CASE(96) VALU_CASE(128) VALU_CASE(160) VALU_CASE(192) VALU_CASE(224) VALU_CASE(256)
 #undef VALU_CASE
     default: return hipErrorInvalidValue;
@@ -222,6 +226,7 @@ int attn_valu_rows_per_block(int d) { return valu_rows(d); }
 
 hipError_t launch_attn_valu(const DevState& s, const AttnArgs& a, hipStream_t st, hipEvent_t ev0,
                             hipEvent_t ev1) {
+  if (a.prefix_o && (a.splits > 1 || a.partial)) return hipErrorInvalidValue;
   const dim3 grid(s.T * a.n_layers * s.Hkv * a.row_blocks * a.splits);
   if (s.dtype == TD_F32) return launch_t<float>(s, a, grid, st, ev0, ev1);
   return launch_t<__bf16>(s, a, grid, st, ev0, ev1);
