@@ -162,7 +162,11 @@ td_status td_init_prompt(td_ctx* ctx, const int32_t* h_prompt_len, const int32_t
  * otherwise, and after trie_store_kv of every layer of the call, d_k_new/d_v_new must be NULL
  * (else TD_EINVAL).  A call over some layers that trie_store_kv has stored and some that are
  * still due needs them, and stores them for all of its layers: they replace trie_store_kv's
- * rows.  fp32 accumulation; out rows of beams >= n_live are zeroed.  scale is normally 1/sqrt(d). */
+ * rows.  fp32 accumulation; out rows of beams >= n_live are zeroed.  scale is normally 1/sqrt(d).
+ * In bf16 at head_dim 64, 96 and 128 the K and V of every stored node (dead ones too) must be
+ * finite, here and in trie_tree_attn: a hidden node weighs 0, and 0 times an infinity is a NaN in
+ * rows that do not see it.  (In the other kernels, and in a shared prefix's positions, what a row
+ * does not see may hold anything, and so may slots without a node.) */
 td_status trie_attn_decode(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, const void* d_q,
                            const void* d_k_new, const void* d_v_new, void* d_out, float scale,
                            hipStream_t stream);
