@@ -567,13 +567,12 @@ __global__ __launch_bounds__(kMergeThreads) void k_prefix_merge(DevState s, Pref
   t8 y;
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] = (T)(live && L != 0.0f ? O[e] * inv : 0.0f);
-  *reinterpret_cast<t8*>(static_cast<T*>(a.out) + ((((size_t)li * a.tries + t) * a.q_stride + a.q0 + j) * s.Hq + head) * D + c) = y;
+  *reinterpret_cast<t8*>(static_cast<T*>(a.out) + (size_t)row * D + c) = y;
 }
 
 }  // namespace
 
-int prefix_rows_per_block(const DevState& s, long rows) {
-  (void)s;
+int prefix_rows_per_block(long rows) {
   return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
 }
 
@@ -590,7 +589,7 @@ int prefix_splits(const DevState& s, long units, long keys, long most) {
 }
 
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
-  const int rpb = prefix_rows_per_block(s, (long)a.tries * a.per_trie * (s.Hq / s.Hkv));
+  const int rpb = prefix_rows_per_block((long)a.tries * a.per_trie * (s.Hq / s.Hkv));
   if (a.trie_splits > 0 && (a.rows != PrefixRows::kLeaves || s.dtype != TD_BF16 || !mfma_head_dim(s.D))) return hipErrorInvalidValue;
   if (s.dtype == TD_F32) return launch_prefix32(s, a, rpb, st, ev0, ev1);
   switch (s.D) {
@@ -603,14 +602,14 @@ hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st,
   return hipGetLastError();
 }
 
-hipError_t launch_prefix_merge(const DevState& s, const PrefixMergeArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
+hipError_t launch_prefix_merge(const DevState& s, const PrefixMergeArgs& a, hipStream_t st, hipEvent_t ev1) {
   const long items = (long)a.n_layers * a.tries * a.per_trie * s.Hq * (s.D / 8);
   const int n = (a.trie ? a.trie_splits : 0) + a.prefix_splits;
   const int tp = n > 16 ? 4 : n > 8 ? 2 : 1;  // lanes per output chunk: 8 records each
   if (items * tp >= (1l << 31)) return hipErrorInvalidValue;  // (a workspace of records is far smaller)
   const dim3 grid((items * tp + kMergeThreads - 1) / kMergeThreads), block(kMergeThreads);
 #define LAUNCH_MERGE(T, TP) \
-  hipExtLaunchKernelGGL((k_prefix_merge<T, TP>), grid, block, 0, st, ev0, ev1, 0, s, a, (uint32_t)items)
+  hipExtLaunchKernelGGL((k_prefix_merge<T, TP>), grid, block, 0, st, nullptr, ev1, 0, s, a, (uint32_t)items)
   if (s.dtype == TD_F32) tp == 4 ? LAUNCH_MERGE(float, 4) : tp == 2 ? LAUNCH_MERGE(float, 2) : LAUNCH_MERGE(float, 1);
   else tp == 4 ? LAUNCH_MERGE(__bf16, 4) : tp == 2 ? LAUNCH_MERGE(__bf16, 2) : LAUNCH_MERGE(__bf16, 1);
 #undef LAUNCH_MERGE

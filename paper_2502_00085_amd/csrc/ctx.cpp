@@ -24,14 +24,8 @@ constexpr long kOneRoundWgs = 256;  // attention WGs that run at once (one per C
 
 template <typename T>
 hipError_t alloc(td_ctx* c, T** p, size_t n) {
-  void* q = nullptr;
-  const size_t bytes = n * sizeof(T) > 0 ? n * sizeof(T) : 16;
-  hipError_t e = hipMalloc(&q, bytes);
-  if (e != hipSuccess) return e;
-  c->allocs.push_back(q);
-  e = hipMemset(q, 0, bytes);
-  *p = static_cast<T*>(q);
-  return e;
+  const hipError_t e = td::reserve(c, p, n);
+  return e == hipSuccess ? hipMemset(*p, 0, n * sizeof(T)) : e;
 }
 
 td::TrieShape shape_of(const td::DevState& s) { return {s.b, s.W, s.G, s.cap}; }

@@ -41,6 +41,16 @@ namespace td {
 // Sets the context's message (that of td_error_string(NULL) without one) and returns st.
 td_status fail(td_ctx* c, td_status st, const char* fmt, ...) __attribute__((format(printf, 3, 4)));
 td_status hip_fail(td_ctx* c, hipError_t e, const char* what);
+// Device memory of the context, freed by td_destroy.
+template <typename T>
+hipError_t reserve(td_ctx* c, T** p, size_t n) {
+  void* q = nullptr;
+  const hipError_t e = hipMalloc(&q, n * sizeof(T));
+  if (e != hipSuccess) return e;
+  c->allocs.push_back(q);
+  *p = static_cast<T*>(q);
+  return e;
+}
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 // TD_ESTATE unless every trie is initialised.
 td_status check_ready(td_ctx* c);

@@ -11,6 +11,7 @@
 using td::aligned16;
 using td::fail;
 using td::hip_fail;
+using td::reserve;
 
 namespace {
 
@@ -36,16 +37,6 @@ td_status other_device(td_ctx* c) {
   if (e != hipSuccess) return hip_fail(c, e, "hipGetDevice");
   if (d != c->device) return fail(c, TD_EINVAL, "the context lives on device %d, the current one is %d", c->device, d);
   return TD_OK;
-}
-
-template <typename T>
-hipError_t reserve(td_ctx* c, T** p, size_t n) {
-  void* q = nullptr;
-  const hipError_t e = hipMalloc(&q, n * sizeof(T));
-  if (e != hipSuccess) return e;
-  c->allocs.push_back(q);
-  *p = static_cast<T*>(q);
-  return e;
 }
 
 // The arguments that the two stores share.
@@ -100,7 +91,7 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   a.q_stride = q_max;
   a.scale_log2 = scale_log2;
   const long rows = (long)s.T * qn * (s.Hq / s.Hkv);
-  const int rpb = prefix_rows_per_block(s, rows);
+  const int rpb = prefix_rows_per_block(rows);
   a.row_blocks = (int)((rows + rpb - 1) / rpb);
   const long keys = s.W > 0 ? std::min(c->prefix_length, s.W) : c->prefix_length;
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * s.T * qn * s.Hq));
@@ -152,8 +143,8 @@ hipError_t prefix_merge(td_ctx* c, bool nodes, const AttnArgs& a, int splits, in
   m.rows = nodes ? PrefixRows::kNodes : PrefixRows::kLeaves;
   m.n_layers = a.n_layers;
   m.tries = c->dev.T;
-  m.per_trie = m.q_stride = q_max;
-  return launch_prefix_merge(c->dev, m, st, nullptr, ev1);
+  m.per_trie = q_max;
+  return launch_prefix_merge(c->dev, m, st, ev1);
 }
 
 }  // namespace td
@@ -297,7 +288,7 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
   if ((int64_t)n * G > (1 << 24)) return fail(c, TD_EINVAL, "n must be at most 2^24 / (Hq / Hkv)");
   if (td_status r = other_device(c)) return r;
   const long rows = (long)n * G;
-  const int rpb = td::prefix_rows_per_block(s, rows), blocks = (int)((rows + rpb - 1) / rpb);
+  const int rpb = td::prefix_rows_per_block(rows), blocks = (int)((rows + rpb - 1) / rpb);
   // (as many layers per launch as its grid holds)
   const int lc = (int)std::max(1l, std::min<long>(n_layers, (1l << 22) / ((long)s.Hkv * blocks)));
   const size_t layer = (size_t)n * s.Hq * s.D * (s.dtype == TD_F32 ? 4 : 2);
@@ -337,8 +328,8 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
       m.rows = td::PrefixRows::kChunk;
       m.n_layers = a.n_layers;
       m.tries = 1;
-      m.per_trie = m.q_stride = n;
-      e = td::launch_prefix_merge(s, m, st, nullptr, last);
+      m.per_trie = n;
+      e = td::launch_prefix_merge(s, m, st, last);
     }
   }
   if (e != hipSuccess) return hip_fail(c, e, "trie_prefix_attn launch");

@@ -36,7 +36,7 @@ struct PrefixArgs {
 };
 
 // Query rows of a workgroup for a pass of this many rows per KV head.
-int prefix_rows_per_block(const DevState& s, long rows);
+int prefix_rows_per_block(long rows);
 // Splits of `keys` keys for `units` (layer, KV head, row block) units, at most `most`.
 int prefix_splits(const DevState& s, long units, long keys, long most);
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1);
@@ -44,7 +44,7 @@ hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_
                            hipEvent_t ev1);
 
 // Merges a pass's records with those of the tries (attention partials of `splits` splits in blocks of
-// block_rows rows, null: none) into out.
+// block_rows rows, null: none) into out [n_layers][tries][per_trie][Hq][D].
 struct PrefixMergeArgs {
   const float* prefix_o;
   const float2* prefix_ml;
@@ -53,9 +53,9 @@ struct PrefixMergeArgs {
   int trie_splits, block_rows, row_blocks;
   void* out;
   PrefixRows rows;
-  int n_layers, tries, per_trie, q0, q_stride;
+  int n_layers, tries, per_trie;
 };
-hipError_t launch_prefix_merge(const DevState& s, const PrefixMergeArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1);
+hipError_t launch_prefix_merge(const DevState& s, const PrefixMergeArgs& a, hipStream_t st, hipEvent_t ev1);
 
 // Rotated K/V (and queries) into the pools of the tries or the pages of the prefix.
 struct StoreArgs {
