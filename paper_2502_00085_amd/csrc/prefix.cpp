@@ -101,10 +101,15 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   *tries = false;
   if (trie_nodes > 0) {
     // the tries' own nodes in the same launch, where all of its WGs run at once, none has more than
-    // kTrieTiles tiles of a trie, and the pass itself is short.  A step of 4 x 8 beams over 4,096 positions
-    // and 272 nodes each, a layer: 21.5 us, with a launch of its own for the tries 29.5; 2 x 4 beams over
-    // 50,001 positions (32 KV heads, 49 tiles per WG): 123.5 and 120.8.  A trie's WG has 3 of its tiles,
-    // which take about as long as the 4 that a WG of the prefix has at least (2: 22.3 us; 6: 25.7).
+    // kTrieTiles tiles of a trie, and the pass itself is short.  Measured over 210 shapes (1 to 16 tries of 2 to
+    // 32 beams and 40 to 5,000 nodes, 64 to 50,000 positions, d = 64 to 128; graphs of one-layer calls): within
+    // these limits 21 % less time than with launches of their own (4 x 8 beams of 266 nodes over 4,096
+    // positions 22.1 us a layer against 30.3), at worst 4 % more (2 x 32 of 229 over 64: 21.9, 21.1).  Past
+    // kTrieTiles, 11 % less to 12 % more.  The other two limits keep away from what was not measured, calls of
+    // many layers, and cost one-layer calls past them 7 % (2 x 4 beams of 404 nodes over 50,000 positions, 32 KV
+    // heads, 49 tiles of the prefix per WG: 117.8, 127.2).
+    // A trie's WG has 3 of its tiles, which take about as long as the 4 that a WG of the prefix has at least:
+    // over 160 of these shapes 1 or 2 took 1.4 % less in the mean, 4 took 4 % more, 6 8 %, 8 13 %.
     const long wgs = (long)n_layers * s.Hkv * a.row_blocks * a.splits, tiles = (trie_nodes + 63) / 64;
     const long blocks = (qn * (s.Hq / s.Hkv) + rpb - 1) / rpb, units = (long)n_layers * s.T * s.Hkv * blocks;
     const long ts = std::max(1l, std::min({(tiles + 2) / 3, 256 / units, fit - a.splits}));
