@@ -7,7 +7,7 @@ import torch
 
 import paper_2502_00085_amd.binding as B
 from gpu_harness import log
-from prefix_ref import HALF_F32, Prefix, attend, check, half_step, path_of
+from prefix_ref import HALF_F32, Prefix, attend, check, half_step, path_of, turn, turn_error
 from test_gpu_prefix_attn import Batch, randn
 
 pytestmark = pytest.mark.gpu
@@ -259,3 +259,65 @@ def test_a_row_alone():
     a, _ = attend(q, k, v, seen, 0.2, torch.bfloat16)
     c, _ = attend_all(q.cuda(), k.cuda(), v.cuda(), seen.cuda(), 0.2, torch.bfloat16)
     assert float((a - c.cpu()).abs().max()) < 1e-12
+
+
+def test_graph_behind_a_shorter_table():
+    """Captured calls, replayed when the table has become shorter or the prefix is detached: positions that
+    it no longer has are not stored (the sticky status says so) and not seen, nodes are at their depths."""
+    gen, rng, dt = torch.Generator().manual_seed(21), np.random.default_rng(21), torch.bfloat16
+    dec = B.TrieDecoder(1, 2, 40, 50, 1, 4, 2, 64)
+    dec.init_prompt([9], torch.zeros((1, 9), dtype=torch.int32, device="cuda"))
+    full = Prefix(gen, rng, 1, 2, 64, dt, 100, 16)
+    full.attach(dec)
+    k, v, q = randn(gen, (1, 30, 2, 64), dt), randn(gen, (1, 30, 2, 64), dt), randn(gen, (1, 30, 4, 64), dt)
+    lk, lq = randn(gen, (1, 1, 2, 2, 64), dt), randn(gen, (1, 1, 2, 4, 64), dt)
+    rope = B.Rope(torch.linspace(1.0, 0.01, 32, device="cuda"))
+    rot, out, lrot, lout = torch.empty_like(q), torch.empty_like(q), torch.empty_like(lq), torch.empty_like(lq)
+
+    def step():
+        dec.prefix_store(0, 1, 40, k, v, q, rot, rope)
+        dec.prefix_attn(0, 1, 40, rot, out, 0.125)
+        dec.store_kv(0, 1, lk, lk, lq, lrot, rope)
+        dec.attn_decode(0, 1, lrot, None, None, lout, 0.125)
+
+    step()
+    torch.cuda.synchronize()
+    assert dec.status() == 0
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        step()
+    for room in (48, 16, 0, 112):
+        if room:
+            dec.set_prefix(full.k, full.v, full.pages[:room // 16], min(100, room))
+        else:
+            dec.set_prefix(None)
+        full.k.fill_(0.5)
+        full.v.copy_(randn(gen, tuple(full.v.shape), dt))
+        for x in (rot, out, lrot, lout):
+            x.fill_(9.0)
+        before = full.v.clone()
+        for _ in range(2):
+            graph.replay()
+        n = min(30, max(0, room - 40))  # positions of the call that the table still has
+        assert dec.status() == (0 if n == 30 else B.TD_EINVAL)
+        assert dec.status() == 0
+        stored = torch.zeros(full.v.shape[:4], dtype=torch.bool, device="cuda")
+        for j in range(n):
+            stored[int(full.pages[(40 + j) // 16]), :, :, (40 + j) % 16] = True
+            assert torch.equal(full.v[int(full.pages[(40 + j) // 16]), 0, :, (40 + j) % 16], v[0, j])
+        assert torch.equal(full.v[~stored], before[~stored])
+        assert bool((rot[:, n:] == 0).all()) and not bool((rot[:, :n] == 0).all(-1).any())
+        kk, vv = (torch.stack([x[int(full.pages[p // 16]), 0, :, p % 16] for p in range(room)], 1) if room else x[0, 0][:, :0] for x in (full.k, full.v))
+        for j in (0, 7, 8, 29):
+            m = min(40 + j + 1, room)
+            if m == 0:
+                assert bool((out[0, j] == 0).all())
+                continue
+            want, tol = attend(rot[0, j:j + 1], kk[:, :m], vv[:, :m], torch.ones(1, m, dtype=torch.bool), 0.125, dt)
+            check(out[0, j:j + 1], want, tol, (room, j))
+        at = min(100, room)
+        ok, ov = (torch.cat([a[:, :at], pool[0, 0, :, :9]], 1) for a, pool in ((kk, dec.k_pool), (vv, dec.v_pool)))
+        want, tol = attend(lrot[0, 0, :1], ok, ov, torch.ones(1, at + 9, dtype=torch.bool), 0.125, dt)
+        check(lout[0, 0, :1], want, tol, room)
+        check(lrot[0, 0, :1], turn(lq[0, 0, :1], [at + 8], rope.freq, False), turn_error(lq[0, 0, :1], rope.freq, False, dt), room)
+    dec.close()
