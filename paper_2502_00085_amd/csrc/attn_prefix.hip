@@ -13,17 +13,17 @@
 // rows come from the pages of a paged cache: a tile lies in one page of 64 keys or more, or in up to
 // four smaller ones, whose numbers are loaded a tile ahead by scalar loads.
 //
-// What bounds it, by the rows that share a key (times of one MI355X, d = 128 unless stated):
-//   * few rows: HBM.  8 rows per KV head (32 KV heads, d = 96) over 50,001 keys: 106 to 111 us, 5.5 to
-//     5.8 TB/s of reads.  Below some 4,000 keys per KV head a launch is a chain of latencies: 128 rows over 4,096
-//     keys of 8 KV heads, with the tries' own nodes, 17.0 us (its 17 MB take 3.4).
-//   * many rows: the clock under matrix load.  1,024 rows of 8 KV heads over 8,192 keys of 4 layers: 151 to 167 us,
-//     828 to 911 TFLOP/s; the causal pass of 2,048 tokens from position 6,144: 240 to
-//     245 us, 983 to 1,002 TFLOP/s (a
-//     library product of 8,192^3 makes 1,121 here).  There the card runs at 1.9 of its 2.4 GHz, the
-//     matrix pipe busy for half of the clocks, the vector ALU (the exponentials) as long, LDS a quarter.
-//     Each of the two waves of a SIMD fills the other's gaps: a loop that interleaves one half's weights
-//     with its neighbours' products by hand took the same time to 0.3 %.
+// What bounds it, by the rows that share a key (one MI355X, d = 128 unless stated; kernel trace, mean of
+// passes once the clocks have settled, in brackets the least):
+//   * few rows: HBM.  8 rows per KV head (32 KV heads, d = 96) over 50,001 keys: 112 (108) us, 5.5 (5.7)
+//     TB/s of reads.  Below some 4,000 keys per KV head a launch is a chain of latencies: 128 rows over 4,096
+//     keys of 8 KV heads, with the tries' own nodes, 16.5 (14.6) us (its 17 MB take 3.4).
+//   * many rows: the clock under matrix load.  1,024 rows of 8 KV heads over 8,192 keys of 4 layers: 160 (154)
+//     us, 859 (892) TFLOP/s; the causal pass of 2,048 tokens from position 6,144: 249 (246) us, 966 (976)
+//     TFLOP/s, and 244 us, 984, without the trace (a library product of 8,192^3 makes 1,121 here).  There the
+//     card runs at 2.0 to 2.1 of its 2.4 GHz, the matrix pipe busy for half of the CUs' clocks, the vector ALU
+//     (the exponentials) as long, LDS a quarter.  Each of the two waves of a SIMD fills the other's gaps: a
+//     loop that interleaves one half's weights with its neighbours' products by hand took the same time to 0.3 %.
 // Tried and not kept: four tile buffers (16,384 keys in 8 splits: 60 us against 48); 8 waves, of two
 // groups of keys, per 128 rows (8,192 keys, 1,024 rows: 55 us against 50); a fixed order of products and
 // LDS reads (1.5 % slower); 64 rows per wave, one wave per SIMD (568 us against 480 for two causal layers).

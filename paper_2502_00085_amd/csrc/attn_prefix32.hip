@@ -13,8 +13,8 @@
 // at d = 128), far longer than its loads take: one LDS buffer per WG, and two WGs per CU, one of which
 // multiplies while the other loads.  (A tile's V requested during its scores and the next one's K
 // during its output measured 5 to 10 % slower; two accumulators in turn, no faster.)  1,024 rows of 8 KV
-// heads over 4,096 keys at d = 128, 180 us: 96 TFLOP/s of the 133 at that launch's clock (matrix pipe
-// busy 72 % of the CUs' time, by its counter).
+// heads over 4,096 keys at d = 128, 176 us (the least 173): 98 TFLOP/s of the 151 that a library product makes
+// (matrix pipe busy 71 % of the CUs' clocks, 64 % of the launch's).
 #include "attn_prefix.h"
 
 namespace td {

@@ -9,9 +9,9 @@
 // The angle of a far position needs more than fp32: p f_i in turns, in 64 bits, less whole turns;
 // the sine and cosine of the rest in fp32, once per (row, pair), in LDS for all of the row's heads.
 //
-// What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape (201 MB in and out) in 39 to 43 us,
-// 4.7 to 5.1 TB/s, as a copy; with few rows one launch's latency (the leaves of 16 tries of 16 beams, 6.3
-// MB, 3.9 to 4.4 us).  Rows are read and written once; up to 8 of one layer share a WG, so that the
+// What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape (201 MB in and out) in 43.4 us (the
+// least 38.1), 4.6 TB/s (5.3; a copy's 5.0); with few rows one launch's latency (the leaves of 16 tries of 16
+// beams, 6.3 MB, 4.3 us; the least 4.1).  Rows are read and written once; up to 8 of one layer share a WG, so that the
 // angles are computed once for the 32 to 48 heads of a row.
 #include <algorithm>
 

@@ -317,8 +317,9 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
     a.records = a.splits = td::prefix_splits(s, units, keys, std::max(1l, fit));
     a.xcd_group = blocks > 1 && ((long)a.n_layers * s.Hkv * a.splits) % 8 == 0;
     // Two WGs per CU at once, and no third: a long block beside a short one.  2,048 tokens of 32 heads (8
-    // KV heads, d = 128) from position 0: 58 -> 54.5 us a layer, from 6,144: 259 -> 254; where fewer CUs have
-    // two (1,500 tokens) 42 -> 41.3.  With more WGs the longest first fill the CUs evenly by themselves.
+    // KV heads, d = 128) from position 0: 57.5 -> 53.7 us a layer, from 6,144: 254 -> 247.5 (graphs in turn);
+    // where fewer CUs have two (1,500 tokens) 42.4 -> 41.4 from 0, 210.4 and 210.7 from 6,144.  With more WGs the
+    // longest first fill the CUs evenly by themselves.
     a.pair_blocks = s.D <= 128 && units * a.splits > kOneRound / 2 && units * a.splits <= kOneRound;
     a.part_o = a.splits > 1 ? c->prefix_o : nullptr;
     a.part_ml = c->prefix_ml;
