@@ -114,7 +114,8 @@ def draw(rng):
         c["queries"] = c["prompt"]
     elif kind == "queries":
         c["queries"] = _log_int(rng, 1, 40)
-    c["prompt"] = max(1, min(c["prompt"], int((1.5e8 if kind != "prompts" else 1.4e8 / (1 + heads / (2 * kv)) * 1.5) / (row * c["tries"])) - c["steps"] * c["beams"]))
+    most = 1.5e8 if kind in ("leaves", "decode") else 2.1e8 / (1 + heads / (2 * kv))  # bytes of K + V
+    c["prompt"] = max(1, min(c["prompt"], int(most / (row * c["tries"])) - c["steps"] * c["beams"]))
     c["prompt_min"] = max(1, int(c["prompt"] * rng.choice([1.0, 0.3])))
     c["length"] = max(1, min(c["length"], int(2.0e8 / row)))
     if kind in ("decode", "queries"):
