@@ -17,10 +17,11 @@
  * the same attention with any set of stored nodes as queries (a prefill, or draft nodes).
  *
  * Requests that begin alike (a system prompt, examples, a document) can share that beginning:
- * td_set_prefix attaches a prefix in a paged cache to every trie of the context, trie_prefix_store
- * and trie_prefix_attn are its own prefill, and the attention of the tries then runs over the
+ * td_set_prefix attaches a prefix in a paged cache to every trie of the context (td_set_prefix4: one
+ * in 4 bits), trie_prefix_store and trie_prefix_attn are its own prefill, and the attention of the tries then runs over the
  * prefix, once for all of them, and over their own nodes.  trie_store_kv rotates queries and keys
- * to the nodes' positions and stores their rows.
+ * to the nodes' positions and stores their rows; trie_store_kv_axes and trie_prefix_store_axes do so
+ * for positions of several axes (images, video).
  *
  * Memory.  The caller owns every tensor (K/V pools, queries, outputs, logits and
  * selections) as device memory; PyTorch tensors are the intended source.  The library
@@ -214,6 +215,35 @@ typedef struct {
  * replayed; one captured without stays without. */
 td_status td_set_prefix(td_ctx* ctx, const td_prefix* prefix);
 
+/* A prefix in 4 bits, a little over a quarter of the bf16 pages' memory (17 bytes for 32 elements): each block
+ * of 32 elements of a row has a scale byte x, its unit 2^(x - 127) (255: the block is NaN), and each element 4
+ * bits, a sign (bit 3) and the code of 0, 0.5, 1, 1.5, 2, 3, 4 or 6 units (bits 2 .. 0); element 2i is in the
+ * low half of byte i (the open MXFP4 format).  The other fields are those of td_prefix. */
+typedef struct {
+  void* k_pages;               /* device [n_pages][L][Hkv][page_size][d / 2] bytes, 16-byte aligned  */
+  void* v_pages;
+  void* k_scales;              /* device [n_pages][L][Hkv][page_size][d / 32] bytes                   */
+  void* v_scales;
+  int32_t n_pages;
+  int32_t page_size;
+  const int32_t* h_page_table;
+  int32_t n_table;
+  int32_t length;
+} td_prefix4;
+
+/* td_set_prefix with pages in 4 bits (NULL: detach), for contexts of either type and every head dim.  One
+ * prefix is attached at a time, of either kind; trie_prefix_store, trie_prefix_load, trie_prefix_attn and the
+ * tries' attention then work on 4-bit positions: trie_prefix_store rounds K (rotated, in 64 bits) and V to 4
+ * bits once; the attention multiplies the values that the stored rows stand for, which bf16 holds exactly
+ * (past fp32's range: infinite), in the context's type as ever.  The tries' own nodes stay in the context's type.
+ *   Rounding.  m = 2^k f (1 <= f < 2), the largest size of a block, has the unit 2^(k - 2), or 2^(k - 1) where f
+ *   >= 1.75, within 2^-125 and 2^125 (a block of zeros 2^-125); an element is the nearest of the eight sizes of
+ *   units, ties to the even code, past 6 as 6.  A block with an infinity (also: past fp32's range after the
+ *   rotation) or a NaN gets scale 255.
+ * A captured call is of the kind attached when it was captured.  Replayed with a prefix of the other kind
+ * attached it sees no position of it, and sets the sticky device status TD_EINVAL. */
+td_status td_set_prefix4(td_ctx* ctx, const td_prefix4* prefix);
+
 /* A rotary position embedding: pair i of a head's first `dim` elements turns by position *
  * d_freq[i]: (x, y) -> (x cos - y sin, y cos + x sin); the elements past dim are copied. */
 typedef struct {
@@ -221,6 +251,20 @@ typedef struct {
   int32_t dim;          /* a multiple of 16 in [16, d]                                             */
   int32_t interleaved;  /* 0: pair i is elements (i, i + dim / 2); 1: (2i, 2i + 1)                  */
 } td_rope;
+
+/* A rotation by positions of several axes (time, height, width of images and video): pair i of `rope` turns by
+ * the position of axis h_axis[i].  A row's positions are those of d_pos, or (NULL) its own on every axis -
+ * S + depth of a node, pos + j of a token of the prefix - plus d_shift of its trie and axis (text behind images,
+ * which take fewer positions than tokens; NULL: none).  They turn rows only: what a query sees, and the window,
+ * go by where rows are stored. */
+typedef struct {
+  td_rope rope;
+  int32_t n_axes;              /* 1 .. 4                                                            */
+  const uint8_t* h_axis;       /* host [rope.dim / 2]: the axis of each pair, in [0, n_axes); copied */
+  const int32_t* d_pos;        /* device [rows of a layer][n_axes], or NULL: rows are those of q, k, v */
+                               /*   ([n], [T][q_max]); read when the call runs                       */
+  const int32_t* d_shift;      /* device [T][n_axes], or NULL ([1][n_axes] for the prefix); not both  */
+} td_rope_axes;
 
 /* Store n <= 2^26 tokens of the prefix at positions pos .. pos + n - 1 (inside the table; `length`
  * plays no part), for layers [layer_begin, +n_layers): K rotated to its position (rope NULL: as it is) and V
@@ -232,6 +276,17 @@ typedef struct {
 td_status trie_prefix_store(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n,
                             const td_rope* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
                             const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t stream);
+
+/* The same with positions of several axes (rope NULL: no rotation). */
+td_status trie_prefix_store_axes(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n,
+                                 const td_rope_axes* rope, const void* d_q, int64_t q_stride, const void* d_k,
+                                 int64_t k_stride, const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t stream);
+
+/* Rows of the prefix back, as the values that are stored (K rotated): positions pos .. pos + n - 1, n <= 2^26
+ * (inside the table; `length` plays no part), into d_k and d_v [nl][n][Hkv][d], desc.dtype; either may be NULL.
+ * From 4-bit pages the values are exact.  Needs an attached prefix (else TD_ESTATE), but no prompts. */
+td_status trie_prefix_load(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n, void* d_k,
+                           void* d_v, hipStream_t stream);
 
 /* Causal attention of n tokens of the prefix (its prefill, whole or in chunks): the query of token
  * j, at position pos + j, attends to the stored positions p <= pos + j with pos + j - p < W when a
@@ -257,6 +312,11 @@ td_status trie_prefix_attn(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, i
 td_status trie_store_kv(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t q_max, const int32_t* d_qslots,
                         const td_rope* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
                         const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t stream);
+
+/* The same with positions of several axes (rope NULL: no rotation). */
+td_status trie_store_kv_axes(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t q_max, const int32_t* d_qslots,
+                             const td_rope_axes* rope, const void* d_q, int64_t q_stride, const void* d_k,
+                             int64_t k_stride, const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t stream);
 
 /* Phases of a decode step that td_set_kernel_events can time. */
 typedef enum {

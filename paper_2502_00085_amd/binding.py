@@ -50,8 +50,19 @@ class TdPrefix(ctypes.Structure):
                 ("n_table", ctypes.c_int32), ("length", ctypes.c_int32)]
 
 
+class TdPrefix4(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("h_page_table", ctypes.POINTER(ctypes.c_int32)), ("n_table", ctypes.c_int32), ("length", ctypes.c_int32)]
+
+
 class TdRope(ctypes.Structure):
     _fields_ = [("d_freq", ctypes.c_void_p), ("dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class TdRopeAxes(ctypes.Structure):
+    _fields_ = [("rope", TdRope), ("n_axes", ctypes.c_int32), ("h_axis", ctypes.POINTER(ctypes.c_uint8)),
+                ("d_pos", ctypes.c_void_p), ("d_shift", ctypes.c_void_p)]
 
 
 class TdState(ctypes.Structure):
@@ -102,6 +113,11 @@ def lib() -> ctypes.CDLL:
         L.trie_prefix_store.argtypes = [vp, i32, i32, i32, i32, rope, vp, i64, vp, i64, vp, i64, vp, vp]
         L.trie_store_kv.argtypes = [vp, i32, i32, i32, vp, rope, vp, i64, vp, i64, vp, i64, vp, vp]
         L.trie_prefix_attn.argtypes = [vp, i32, i32, i32, i32, vp, vp, f32, vp]
+        L.td_set_prefix4.argtypes = [vp, ctypes.POINTER(TdPrefix4)]
+        axes = ctypes.POINTER(TdRopeAxes)
+        L.trie_prefix_store_axes.argtypes = [vp, i32, i32, i32, i32, axes, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.trie_store_kv_axes.argtypes = [vp, i32, i32, i32, vp, axes, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.trie_prefix_load.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp]
         L.td_error_string.argtypes = [vp]
         L.td_error_string.restype = ctypes.c_char_p
         L.beam_topk_static.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
@@ -123,7 +139,8 @@ def lib() -> ctypes.CDLL:
                      "beam_logsoftmax_topk", "beam_topk_append", "beam_topk_static", "td_read_probe", "trie_append_prune",
                      "td_read_state", "td_load_state",
                      "td_get_status", "td_set_kernel_events", "td_read_finished", "trie_tree_attn",
-                     "td_set_prefix", "trie_prefix_store", "trie_store_kv", "trie_prefix_attn", "bbs_create", "bbs_destroy",
+                     "td_set_prefix", "trie_prefix_store", "trie_store_kv", "trie_prefix_attn", "td_set_prefix4",
+                     "trie_prefix_store_axes", "trie_store_kv_axes", "trie_prefix_load", "bbs_create", "bbs_destroy",
                      "bbs_init_prompt", "batch_beam_attn_decode", "batch_beam_logsoftmax_topk",
                      "batch_beam_reorder", "bbs_current_cache", "bbs_read_beams", "bbs_get_status"):
             getattr(L, name).restype = ctypes.c_int32
@@ -232,6 +249,44 @@ class Rope:
         self.c = TdRope(freq.data_ptr(), 2 * freq.numel(), int(bool(interleaved)))
 
 
+class RopeAxes:
+    """A rotary embedding by positions of several axes (td_rope_axes): freq and interleaved as in Rope, axis the
+    axis (0 .. 3) of each pair.  The positions come with each call."""
+
+    def __init__(self, freq, axis: Sequence[int], interleaved: bool = False):
+        self.rope = Rope(freq, interleaved)
+        axis = np.asarray(axis)
+        if axis.shape != (freq.numel(),) or not np.isin(axis, (0, 1, 2, 3)).all():
+            raise ValueError("axis must hold an axis in 0 .. 3 for each pair")
+        self.axis = np.ascontiguousarray(axis, dtype=np.uint8)
+        self.n_axes = int(axis.max()) + 1 if axis.size else 1
+
+    def c(self, rows: Sequence[int], tries: int, positions, shift):
+        """td_rope_axes of a call whose rows have the shape ``rows``."""
+        import torch
+        for name, t, lead in (("positions", positions, rows), ("shift", shift, (tries,))):
+            if t is None:
+                continue
+            if tuple(t.shape[:-1]) != tuple(lead) or not self.n_axes <= t.shape[-1] <= 4:
+                raise ValueError(f"{name} must be {list(lead)} with {self.n_axes} to 4 axes, got {list(t.shape)}")
+            _ptr(t, torch.int32, None, name)
+        if positions is not None and shift is not None:
+            raise ValueError("pass positions or shift, not both")
+        given = positions if positions is not None else shift
+        n_axes = self.n_axes if given is None else int(given.shape[-1])
+        return TdRopeAxes(self.rope.c, n_axes, self.axis.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8)),
+                          None if positions is None else positions.data_ptr(), None if shift is None else shift.data_ptr())
+
+
+def _rope_call(rope, rows, tries, positions, shift):
+    """(whether the call is the one of several axes, its rope argument)."""
+    if isinstance(rope, RopeAxes):
+        return True, ctypes.byref(rope.c(rows, tries, positions, shift))
+    if positions is not None or shift is not None:
+        raise ValueError("positions and shift go with a RopeAxes")
+    return False, None if rope is None else ctypes.byref(rope.c)
+
+
 def td_set_prefix(ctx, dims: Dims, k_pages, v_pages=None, pages: Sequence[int] = (), length: int = 0):
     """Attach a prefix (k_pages None: detach): k_pages / v_pages [n_pages][L][Hkv][page_size][d] device
     tensors, pages the table (position i lies in page pages[i // page_size])."""
@@ -249,6 +304,27 @@ def td_set_prefix(ctx, dims: Dims, k_pages, v_pages=None, pages: Sequence[int] =
                  int(k_pages.shape[0]), int(k_pages.shape[3]), table.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)),
                  table.size, int(length))
     _check(ctx, lib().td_set_prefix(ctx, ctypes.byref(d)))
+
+
+def td_set_prefix4(ctx, dims: Dims, k_pages, k_scales=None, v_pages=None, v_scales=None, pages: Sequence[int] = (),
+                   length: int = 0):
+    """Attach a prefix in 4 bits (k_pages None: detach): k_pages / v_pages [n_pages][L][Hkv][page_size][d / 2] and
+    k_scales / v_scales [n_pages][L][Hkv][page_size][d / 32], uint8 device tensors; pages as in td_set_prefix."""
+    if k_pages is None:
+        _check(ctx, lib().td_set_prefix4(ctx, None))
+        return
+    import torch
+    if k_pages.dim() != 5 or tuple(k_pages.shape[1:3]) != (dims.L, dims.Hkv) or 2 * k_pages.shape[4] != dims.D:
+        raise ValueError("k_pages must be [n_pages][n_layers][n_kv_heads][page_size][head_dim / 2]")
+    table = np.ascontiguousarray(np.asarray(pages, dtype=np.int32))
+    if table.ndim != 1 or not np.array_equal(table, np.asarray(pages)):
+        raise ValueError("pages must be a sequence of 32-bit integers")
+    n = k_pages.numel()
+    d = TdPrefix4(_ptr(k_pages, torch.uint8, None, "k_pages"), _ptr(v_pages, torch.uint8, n, "v_pages"),
+                  _ptr(k_scales, torch.uint8, n // 16, "k_scales"), _ptr(v_scales, torch.uint8, n // 16, "v_scales"),
+                  int(k_pages.shape[0]), int(k_pages.shape[3]), table.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)),
+                  table.size, int(length))
+    _check(ctx, lib().td_set_prefix4(ctx, ctypes.byref(d)))
 
 
 def _rows(t, dtype, shape, name):
@@ -285,28 +361,46 @@ def _store_rows(dims: Dims, lead, k, v, q, q_out):
 
 
 def trie_prefix_store(ctx, dims: Dims, layer_begin: int, n_layers: int, pos: int, k, v, q=None, q_out=None,
-                      rope: Optional[Rope] = None, stream=None):
+                      rope=None, stream=None, positions=None, shift=None):
     """Store tokens pos, pos + 1, ... of the prefix: k / v [n_layers][n][Hkv][d] (k rotated), q
-    [n_layers][n][Hq][d] rotated to q_out; their rows may be slices of a wider tensor's."""
+    [n_layers][n][Hq][d] rotated to q_out; their rows may be slices of a wider tensor's.  rope: a Rope, or a
+    RopeAxes with positions [n][axes], or shift [1][axes] from the tokens' own (int32 device tensors)."""
     if k is None and q is None:
         raise ValueError("k and v, or q and q_out, must be given")
     n = int((q if k is None else k).shape[1])
     args = _store_rows(dims, (n_layers, n), k, v, q, q_out)
-    _check(ctx, lib().trie_prefix_store(ctx, int(layer_begin), int(n_layers), int(pos), n,
-                                        None if rope is None else ctypes.byref(rope.c), *args, _stream(stream)))
+    axes, turn = _rope_call(rope, (n,), 1, positions, shift)
+    call = lib().trie_prefix_store_axes if axes else lib().trie_prefix_store
+    _check(ctx, call(ctx, int(layer_begin), int(n_layers), int(pos), n, turn, *args, _stream(stream)))
 
 
 def trie_store_kv(ctx, dims: Dims, layer_begin: int, n_layers: int, k, v, q=None, q_out=None,
-                  rope: Optional[Rope] = None, qslots=None, stream=None):
+                  rope=None, qslots=None, stream=None, positions=None, shift=None):
     """Store rows of the live leaves (k / v [n_layers][T][b][Hkv][d]) or of the nodes qslots [T][q_max]
-    (k / v [n_layers][T][q_max][Hkv][d]), rotated to the nodes' positions; q to q_out likewise."""
+    (k / v [n_layers][T][q_max][Hkv][d]), rotated to the nodes' positions; q to q_out likewise.  rope: a Rope, or a
+    RopeAxes with positions [T][b or q_max][axes], or shift [T][axes] from the nodes' own (int32 device tensors)."""
     import torch
     if qslots is not None and (qslots.dim() != 2 or qslots.shape[0] != dims.T):
         raise ValueError("qslots must be [T][q_max]")
     n = dims.b if qslots is None else int(qslots.shape[1])
     args = _store_rows(dims, (n_layers, dims.T, n), k, v, q, q_out)
-    _check(ctx, lib().trie_store_kv(ctx, int(layer_begin), int(n_layers), n, _ptr(qslots, torch.int32, None, "qslots"),
-                                    None if rope is None else ctypes.byref(rope.c), *args, _stream(stream)))
+    axes, turn = _rope_call(rope, (dims.T, n), dims.T, positions, shift)
+    call = lib().trie_store_kv_axes if axes else lib().trie_store_kv
+    _check(ctx, call(ctx, int(layer_begin), int(n_layers), n, _ptr(qslots, torch.int32, None, "qslots"), turn, *args, _stream(stream)))
+
+
+def trie_prefix_load(ctx, dims: Dims, layer_begin: int, n_layers: int, pos: int, k=None, v=None, stream=None):
+    """Rows of the prefix back: positions pos, pos + 1, ... into k / v [n_layers][n][Hkv][d] (either may be None),
+    as the values that are stored."""
+    import torch
+    tdt = torch.float32 if dims.dtype == TD_F32 else torch.bfloat16
+    given = k if k is not None else v
+    if given is None or given.dim() != 4:
+        raise ValueError("k or v must be [n_layers][n][n_kv_heads][head_dim]")
+    n = int(given.shape[1])
+    nk = n_layers * n * dims.Hkv * dims.D
+    _check(ctx, lib().trie_prefix_load(ctx, int(layer_begin), int(n_layers), int(pos), n, _ptr(k, tdt, nk, "k"),
+                                       _ptr(v, tdt, nk, "v"), _stream(stream)))
 
 
 def trie_prefix_attn(ctx, dims: Dims, layer_begin: int, n_layers: int, pos: int, q, out, scale: float, stream=None):
@@ -547,14 +641,23 @@ class TrieDecoder:
         td_set_prefix(self.ctx, self.dims, k_pages, v_pages, pages, length)
         self.prefix_pages = (k_pages, v_pages)  # (kept alive while attached)
 
-    def prefix_store(self, layer_begin, n_layers, pos, k, v, q=None, q_out=None, rope=None, stream=None):
-        trie_prefix_store(self.ctx, self.dims, layer_begin, n_layers, pos, k, v, q, q_out, rope, stream)
+    def set_prefix4(self, k_pages, k_scales=None, v_pages=None, v_scales=None, pages=(), length=0):
+        td_set_prefix4(self.ctx, self.dims, k_pages, k_scales, v_pages, v_scales, pages, length)
+        self.prefix_pages = (k_pages, k_scales, v_pages, v_scales)  # (kept alive while attached)
+
+    def prefix_store(self, layer_begin, n_layers, pos, k, v, q=None, q_out=None, rope=None, stream=None, positions=None,
+                     shift=None):
+        trie_prefix_store(self.ctx, self.dims, layer_begin, n_layers, pos, k, v, q, q_out, rope, stream, positions, shift)
+
+    def prefix_load(self, layer_begin, n_layers, pos, k=None, v=None, stream=None):
+        trie_prefix_load(self.ctx, self.dims, layer_begin, n_layers, pos, k, v, stream)
 
     def prefix_attn(self, layer_begin, n_layers, pos, q, out, scale, stream=None):
         trie_prefix_attn(self.ctx, self.dims, layer_begin, n_layers, pos, q, out, scale, stream)
 
-    def store_kv(self, layer_begin, n_layers, k, v, q=None, q_out=None, rope=None, qslots=None, stream=None):
-        trie_store_kv(self.ctx, self.dims, layer_begin, n_layers, k, v, q, q_out, rope, qslots, stream)
+    def store_kv(self, layer_begin, n_layers, k, v, q=None, q_out=None, rope=None, qslots=None, stream=None, positions=None,
+                 shift=None):
+        trie_store_kv(self.ctx, self.dims, layer_begin, n_layers, k, v, q, q_out, rope, qslots, stream, positions, shift)
 
     def status(self):
         return td_get_status(self.ctx)

@@ -42,6 +42,11 @@ __device__ inline PrefixUnit prefix_unit(const DevState& s, const PrefixArgs& a)
   return u;
 }
 
+// A call captured with a prefix of one kind finds nothing to read where one of the other is attached.
+__device__ inline void prefix_other_kind(const DevState& s, const PrefixHdr& p) {
+  if (p.other != 0 && blockIdx.x == 0 && threadIdx.x == 0) set_status(s.status, kDevEinval);
+}
+
 // Row r of a KV head: its owner, its query's place in q and out (in rows of Hq D elements; a row past
 // the end: the first's), and the keys [lo, hi) it sees (none: a row past the end, an empty query, or
 // a window past the prefix).
@@ -123,6 +128,59 @@ __device__ inline TilePages tile_pages(const PrefixHdr& h, int tile) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) t.p[i] = e[i];
   return t;
+}
+
+// 4-bit tiles.  A block of 32 elements is 16 bytes and a scale byte; the K blocks of a tile of KEYS keys, row
+// after row, are numbers 0 .. KEYS D / 32 - 1, its V blocks follow, and thread tid holds blocks j THREADS +
+// tid (of K or of V alike in a wave, unless KEYS D / 32 is no multiple of 64).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int D, int THREADS, int KEYS>
+struct Blocks4 {
+  static constexpr int BPR = D / 32;         // blocks per row
+  static constexpr int HALF = KEYS * BPR;    // of K (and of V)
+  static constexpr int PER = (2 * HALF + THREADS - 1) / THREADS;
+  // Whether load j of a thread is one of the tile's, and of V; its number among K's, or V's.
+  static __device__ inline int at(int j, int wave) { return j * THREADS + (HALF % 64 == 0 ? wave * 64 : (int)threadIdx.x); }
+  static __device__ inline bool some(int j, int wave) { return 2 * HALF % THREADS == 0 || at(j, wave) < 2 * HALF; }
+  static __device__ inline bool is_v(int j, int wave) { return at(j, wave) >= HALF; }
+  static __device__ inline int number(int j, bool v) { return j * THREADS + (int)threadIdx.x - (v ? HALF : 0); }
+};
+template <int D, int THREADS, int KEYS>
+struct Tile4 {
+  u32x4 x[Blocks4<D, THREADS, KEYS>::PER];
+  uint32_t scale[Blocks4<D, THREADS, KEYS>::PER];
+};
+// Loads the thread's blocks of the tile of keys tb .. (tb / 64's pages: pg); rows past `last` (of the
+// tile) read that row.  head: rows before this (layer, KV head) in a page; wave: threadIdx.x / 64.
+template <int D, int THREADS, int KEYS>
+__device__ inline void fetch4(const PrefixHdr& p, const TilePages& pg, size_t page_rows, size_t head, int tb, int last, int wave,
+                              Tile4<D, THREADS, KEYS>& to) {
+  using B = Blocks4<D, THREADS, KEYS>;
+  const bool one = p.shift >= 6, whole = one && last >= KEYS - 1;  // (uniform)
+  const size_t row0 = (size_t)pg.p[0] * page_rows + head + (one ? tb & ((1 << p.shift) - 1) : 0);
+  // (copies: a choice between members would keep the header in scratch memory)
+  const unsigned char *kx = static_cast<const unsigned char*>(p.k), *vx = static_cast<const unsigned char*>(p.v);
+  const uint8_t *ksc = p.k_scale, *vsc = p.v_scale;
+  const int p0 = pg.p[0], p1 = pg.p[1], p2 = pg.p[2], p3 = pg.p[3];
+#pragma unroll
+  for (int j = 0; j < B::PER; ++j) {
+    if (!B::some(j, wave)) continue;
+    const bool v = B::is_v(j, wave);
+    const unsigned char* x = v ? vx : kx;
+    const uint8_t* sc = v ? vsc : ksc;
+    const uint32_t b = B::number(j, v);
+    if (whole) {
+      to.x[j] = *reinterpret_cast<const u32x4*>(x + row0 * (D / 2) + b * 16);
+      to.scale[j] = (sc + row0 * B::BPR)[b];
+    } else {
+      const int row = min((int)(b / B::BPR), last), n = (tb & 63) + row;
+      const int e = one ? 0 : n >> p.shift;
+      const int page = e == 0 ? p0 : e == 1 ? p1 : e == 2 ? p2 : p3;
+      const size_t at = one ? row0 + row : (size_t)page * page_rows + head + (n & ((1 << p.shift) - 1));
+      to.x[j] = *reinterpret_cast<const u32x4*>(x + at * (D / 2) + b % B::BPR * 16);
+      to.scale[j] = sc[at * B::BPR + b % B::BPR];
+    }
+  }
 }
 
 // The keys [lo, hi) that some row of rows [r0, r0 + n) of a KV head sees, and [all_lo, all_hi) that all

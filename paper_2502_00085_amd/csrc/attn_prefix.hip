@@ -56,11 +56,27 @@ struct PrefixCfg {
   static constexpr int VROT = 8 % NBLK == 0 ? 1 : 4;  // rotations of V rows 8 apart
 };
 
+// Physical chunk of logical chunk c of V row r.  A tile that is unpacked from 4 bits also rotates the chunks
+// within a 64-byte block (which one thread writes, chunk after chunk): the threads of four rows then write to
+// different banks.
+template <int CPR, int NBLK, bool FOUR>
+__device__ inline int v_chunk(int r, int c) {
+  return FOUR ? (c / 4 + r % NBLK) % NBLK * 4 + ((c + r) & 3) : phys_chunk<CPR, NBLK>(r, c);
+}
+template <int CPR, int NBLK, bool FOUR>
+__device__ inline int v_logical(int r, int pc) {
+  return FOUR ? (pc / 4 + NBLK - r % NBLK) % NBLK * 4 + ((pc - r) & 3) : (pc + CPR - 4 * (r % NBLK)) % CPR;
+}
+
 // TRIES: the launch's last WGs take the tries' own nodes (PrefixArgs::trie_splits), for calls so small
 // that a launch of their own would run after this one instead of beside it.  A trie's rows in its
 // pool are one page of nodes; every live row sees its shared prefix, and of the nodes after it those
 // whose ancestor mask holds the row's beam.
-template <int D, int RW, int KW, bool TRIES>
+//
+// FOUR: the prefix is in 4 bits.  Its tiles pass through registers: a thread loads blocks of 32 elements (16
+// bytes and a scale) two tiles ahead and unpacks them, 16 conversions a block, into the tile buffer that the
+// next step reads.  Every value is exact in bf16, and a tile's are converted once for all of its rows.
+template <int D, int RW, int KW, bool TRIES, bool FOUR>
 __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k_attn_prefix(DevState s, PrefixArgs a) {
   using C = PrefixCfg<D, RW, KW>;
   static_assert(2 * C::LOADS < 64, "the wait counter holds a tile's loads");
@@ -72,7 +88,9 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   __shared__ __attribute__((aligned(16))) unsigned char kbuf1[2 * C::HALF], vbuf1[2 * C::HALF];
   __shared__ int wred[4 * RW];
   __shared__ float ml[KW == 2 ? RW * 128 : 1];
-  PrefixHdr p = *s.prefix;
+  using T4 = Tile4<D, C::THREADS, 64>;
+  PrefixHdr p = s.prefix[FOUR ? 1 : 0];
+  prefix_other_kind(s, p);
   const bool trie = TRIES && blockIdx.x >= a.prefix_wgs;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -139,6 +157,7 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   }
   const int lo = all.lo, hi = all.hi;
   // tiles of 64 keys, at multiples of 64: this split's share
+  const bool four = FOUR && !(TRIES && trie);
   const int first = hi > 0 ? lo / 64 : 0, tiles = hi > 0 ? (hi + 63) / 64 - first : 0;
   const int per = (tiles + shares - 1) / shares;
   const int t0 = first + share * per, t1 = max(t0, min(first + tiles, t0 + per));
@@ -168,7 +187,7 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   for (int j = 0; j < C::OFS; ++j) {
     const int c = j * C::THREADS + tid, row = c / C::CPR, pc = c % C::CPR;
     kofs[j] = row * (2 * D) + (pc + C::CPR - row % 32 % C::CPR) % C::CPR * 16;
-    vofs[j] = row * (2 * D) + (pc + C::CPR - 4 * (row % 32 % C::NBLK)) % C::CPR * 16;
+    vofs[j] = row * (2 * D) + v_logical<C::CPR, C::NBLK, FOUR>(row % 32, pc) * 16;
   }
   auto issue = [&](int tile, const TilePages& pg, unsigned char* kdst, unsigned char* vdst) __attribute__((always_inline)) {
     const int tb = tile * 64;
@@ -207,15 +226,53 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     }
   };
 
+  // (4 bits) the tile's blocks of this thread, and the same unpacked into its rows in LDS
+  auto fetch = [&](int tile, const TilePages& pg, T4& to) __attribute__((always_inline)) {
+    fetch4<D, C::THREADS, 64>(p, pg, page_rows, head, tile * 64, hi - 1 - tile * 64, wave, to);
+  };
+  auto unpack = [&](const T4& from, unsigned char* kdst, unsigned char* vdst) __attribute__((always_inline)) {
+    using B = Blocks4<D, C::THREADS, 64>;
+#pragma unroll
+    for (int j = 0; j < B::PER; ++j) {
+      if (!B::some(j, wave)) continue;
+      const bool v = B::is_v(j, wave);
+      const int b = B::number(j, v), row = b / B::BPR, blk = b % B::BPR;
+      const float unit = __uint_as_float(from.scale[j] << 23);
+      unsigned char* const dst = (v ? vdst : kdst) + row * (2 * D);
+      const int k0 = (4 * blk + row % 32) % C::CPR, v0 = (blk + row % 32 % C::NBLK) % C::NBLK * 4;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t w = from.x[j][c];
+        bf16x8 y;
+#define CVT4(I) \
+  { \
+    const bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, I); \
+    y[2 * I] = z[0]; \
+    y[2 * I + 1] = z[1]; \
+  }
+        CVT4(0) CVT4(1) CVT4(2) CVT4(3)
+#undef CVT4
+        const int at = v ? v0 + ((c + row) & 3) : k0 + c < C::CPR ? k0 + c : k0 + c - C::CPR;
+        *reinterpret_cast<bf16x8*>(dst + at * 16) = y;
+      }
+    }
+  };
+
   // the first two tiles go out before anything that waits for the tries
   TilePages next{};
+  T4 ahead, ahead2;  // (4 bits) tiles under way
   if (t0 < t1) {
     const bool main = m0 < m1;
     const int x0 = main ? m0 : cut_tile(0), x1 = main ? m0 + 1 : cut_tile(1);
     const bool two = main ? m0 + 1 < m1 : cut > 1;
     const TilePages pg0 = pages_of(x0), pg1 = pages_of(two ? x1 : x0);
-    issue(x0, pg0, kbuf0, vbuf0);
-    if (two) issue(x1, pg1, kbuf1, vbuf1);
+    if (FOUR && four) {
+      fetch(x0, pg0, ahead);
+      fetch(two ? x1 : x0, pg1, ahead2);
+    } else {
+      issue(x0, pg0, kbuf0, vbuf0);
+      if (two) issue(x1, pg1, kbuf1, vbuf1);
+    }
     if (m0 + 2 < m1) next = pages_of(m0 + 2);
   }
   if (TRIES && trie) {
@@ -239,7 +296,7 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
     for (int dt = 0; dt < C::DT; ++dt) {
       const int n = 8 * x8 + 4 * hh + tm;
       const int c = 4 * dt + 2 * (grp & 1) + (tq >> 1);
-      vread[x8][dt] = (4 * hh + tm) * (2 * D) + phys_chunk<C::CPR, C::NBLK>(n, c) * 16 + 8 * (tq & 1);
+      vread[x8][dt] = (4 * hh + tm) * (2 * D) + v_chunk<C::CPR, C::NBLK, FOUR>(n, c) * 16 + 8 * (tq & 1);
     }
 
   const float scale = a.scale_log2;
@@ -302,14 +359,26 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   };
   auto step = [&](int tile, const unsigned char* kb, const unsigned char* vb, unsigned char* knext,
                   unsigned char* vnext) __attribute__((always_inline)) {
-    // this thread's loads of the tile have landed, then every thread's, and the other buffer is free
-    // (the second tile is on its way already)
-    if (tile == m0 && m0 + 1 < m1) __builtin_amdgcn_s_waitcnt(wait_vm(2 * C::LOADS));
-    else __builtin_amdgcn_s_waitcnt(kWaitVmAll);
-    __syncthreads();
-    if (tile > m0 && tile + 1 < m1) {
-      issue(tile + 1, next, knext, vnext);
-      if (tile + 2 < m1) next = pages_of(tile + 2);
+    if (FOUR && four) {
+      // the tile is unpacked, and the other buffer is free: the next one goes there
+      __syncthreads();
+      if (tile + 1 < m1) {
+        unpack(ahead, knext, vnext);
+        if (tile + 2 < m1) {
+          fetch(tile + 2, next, ahead);
+          if (tile + 3 < m1) next = pages_of(tile + 3);
+        }
+      }
+    } else {
+      // this thread's loads of the tile have landed, then every thread's, and the other buffer is free
+      // (the second tile is on its way already)
+      if (tile == m0 && m0 + 1 < m1) __builtin_amdgcn_s_waitcnt(wait_vm(2 * C::LOADS));
+      else __builtin_amdgcn_s_waitcnt(kWaitVmAll);
+      __syncthreads();
+      if (tile > m0 && tile + 1 < m1) {
+        issue(tile + 1, next, knext, vnext);
+        if (tile + 2 < m1) next = pages_of(tile + 2);
+      }
     }
     f32x16 acc[NH];
 #pragma unroll
@@ -329,6 +398,10 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
       add_values(vb + (KW == 2 ? kw : h) * C::HALF, pb);
     }
   };
+  if (FOUR && four && m0 < m1) {
+    unpack(ahead, kbuf0, vbuf0);
+    ahead = ahead2;
+  }
   for (int t = m0; t < m1; t += 2) {
     step(t, kbuf0, vbuf0, kbuf1, vbuf1);
     if (t + 1 < m1) step(t + 1, kbuf1, vbuf1, kbuf0, vbuf0);
@@ -340,8 +413,17 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
       const bool two = i + 1 < cut;
       const TilePages pg0 = pages_of(cut_tile(i)), pg1 = pages_of(cut_tile(two ? i + 1 : i));
       __syncthreads();  // both buffers are free
-      issue(cut_tile(i), pg0, kbuf0, vbuf0);
-      if (two) issue(cut_tile(i + 1), pg1, kbuf1, vbuf1);
+      if (FOUR && four) {
+        fetch(cut_tile(i), pg0, ahead);
+        fetch(cut_tile(two ? i + 1 : i), pg1, ahead2);
+      } else {
+        issue(cut_tile(i), pg0, kbuf0, vbuf0);
+        if (two) issue(cut_tile(i + 1), pg1, kbuf1, vbuf1);
+      }
+    }
+    if (FOUR && four) {
+      unpack(ahead, kbuf0, vbuf0);
+      unpack(ahead2, kbuf1, vbuf1);
     }
     uint64_t masks[2] = {0, 0};  // (of a trie's nodes) of key `lane` of either tile
     if (TRIES && trie) {
@@ -418,7 +500,7 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
           for (int q4 = 0; q4 < 4; ++q4) {
             // elements 32 dt + 8 q4 + 4 hh .. + 3 of the key's V row
             const bf16x4 x = *reinterpret_cast<const bf16x4*>(
-                vh + n * (2 * D) + phys_chunk<C::CPR, C::NBLK>(n, 4 * dt + q4) * 16 + 8 * hh);
+                vh + n * (2 * D) + v_chunk<C::CPR, C::NBLK, FOUR>(n, 4 * dt + q4) * 16 + 8 * hh);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[dt][4 * q4 + e] += own ? w * (float)x[e] : 0.0f;
           }
@@ -460,11 +542,11 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   prefix_output<__bf16, D>(s, a, u, q, lane, m, lsum, o, reinterpret_cast<float*>(mine));
 }
 
-template <int D>
+template <int D, bool FOUR>
 void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
   const dim3 grid(a.n_layers * s.Hkv * (a.splits * a.row_blocks + a.tries * a.trie_blocks * a.trie_splits));
 #define LAUNCH_PREFIX(RW, KW, TRIES) \
-  hipExtLaunchKernelGGL((k_attn_prefix<D, RW, KW, TRIES>), grid, dim3(64 * RW * KW), 0, st, ev0, ev1, 0, s, a)
+  hipExtLaunchKernelGGL((k_attn_prefix<D, RW, KW, TRIES, FOUR>), grid, dim3(64 * RW * KW), 0, st, ev0, ev1, 0, s, a)
   if constexpr (D == 64 || D == 96 || D == 128) {
     if (a.trie_splits > 0) {
       if (rpb == 32) LAUNCH_PREFIX(1, 2, true);
@@ -593,7 +675,8 @@ hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st,
   if (a.trie_splits > 0 && (a.rows != PrefixRows::kLeaves || s.dtype != TD_BF16 || !mfma_head_dim(s.D))) return hipErrorInvalidValue;
   if (s.dtype == TD_F32) return launch_prefix32(s, a, rpb, st, ev0, ev1);
   switch (s.D) {
-#define PREFIX_CASE(DD) case DD: launch_d<DD>(s, a, rpb, st, ev0, ev1); break;
+#define PREFIX_CASE(DD) \
+  case DD: a.four ? launch_d<DD, true>(s, a, rpb, st, ev0, ev1) : launch_d<DD, false>(s, a, rpb, st, ev0, ev1); break;
     PREFIX_CASE(32) PREFIX_CASE(64) PREFIX_CASE(96) PREFIX_CASE(128)
     PREFIX_CASE(160) PREFIX_CASE(192) PREFIX_CASE(224) PREFIX_CASE(256)
 #undef PREFIX_CASE

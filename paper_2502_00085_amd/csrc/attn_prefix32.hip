@@ -43,13 +43,17 @@ struct Prefix32Cfg {
 template <int CPR>
 __device__ inline int vchunk32(int r, int c) { return (c + 8 * ((r >> 2) & 1)) % CPR; }
 
-template <int D, int RW, int KW>
+// FOUR: the prefix is in 4 bits.  The next tile's blocks of 32 elements are in registers while a tile is
+// multiplied, and are unpacked into the buffer once it has been read.
+template <int D, int RW, int KW, bool FOUR>
 __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void k_attn_prefix32(DevState s, PrefixArgs a) {
   using C = Prefix32Cfg<D, RW, KW>;
+  using T4 = Tile4<D, C::THREADS, C::KEYS>;
   __shared__ __attribute__((aligned(16))) unsigned char kbuf[C::TILE], vbuf[C::TILE];
   __shared__ int wred[4 * RW];
   __shared__ float ml[KW == 2 ? RW * 128 : 1];
-  const PrefixHdr p = *s.prefix;
+  const PrefixHdr p = s.prefix[FOUR ? 1 : 0];
+  prefix_other_kind(s, p);
   const PrefixUnit u = prefix_unit(s, a);
   const int lab = a.layer_begin + u.li;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -136,9 +140,35 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
   };
   auto pages_of = [&](int tile) __attribute__((always_inline)) { return tile_pages(p, (b0 + tile * C::KEYS) / 64); };
 
+  T4 ahead;  // (4 bits) the tile under way
+  auto fetch = [&](int tile, const TilePages& pg) __attribute__((always_inline)) {
+    const int tb = b0 + tile * C::KEYS;
+    fetch4<D, C::THREADS, C::KEYS>(p, pg, page_rows, head, tb, hi - 1 - tb, wave, ahead);
+  };
+  auto unpack = [&]() __attribute__((always_inline)) {
+    using B = Blocks4<D, C::THREADS, C::KEYS>;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int j = 0; j < B::PER; ++j) {
+      if (!B::some(j, wave)) continue;
+      const bool v = B::is_v(j, wave);
+      const int b = B::number(j, v), row = b / B::BPR, blk = b % B::BPR;
+      const float unit = __uint_as_float(ahead.scale[j] << 23);
+      unsigned char* const dst = (v ? vbuf : kbuf) + row * (4 * D);
+      const int rot = v ? 8 * ((row >> 2) & 1) : row % C::CPR;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint32_t w = ahead.x[j][c / 2];
+        const f32x2 y = c % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0);
+        const f32x2 z = c % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1);
+        *reinterpret_cast<f32x4*>(dst + (8 * blk + c + rot) % C::CPR * 16) = f32x4{y[0], y[1], z[0], z[1]};
+      }
+    }
+  };
   TilePages next{};
   if (n_tiles > 0) {
-    issue(0, pages_of(0));
+    if constexpr (FOUR) fetch(0, pages_of(0));
+    else issue(0, pages_of(0));
     if (n_tiles > 1) next = pages_of(1);
   }
   if (known) {
@@ -166,12 +196,21 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
   };
 #pragma unroll 1
   for (int tile = 0; tile < n_tiles; ++tile) {
-    if (tile > 0) {
-      __syncthreads();  // the tile before has been read
-      issue(tile, next);
-      if (tile + 1 < n_tiles) next = pages_of(tile + 1);
+    if constexpr (FOUR) {
+      if (tile > 0) __syncthreads();  // the tile before has been read
+      unpack();
+      if (tile + 1 < n_tiles) {
+        fetch(tile + 1, next);
+        if (tile + 2 < n_tiles) next = pages_of(tile + 2);
+      }
+    } else {
+      if (tile > 0) {
+        __syncthreads();  // the tile before has been read
+        issue(tile, next);
+        if (tile + 1 < n_tiles) next = pages_of(tile + 1);
+      }
+      __builtin_amdgcn_s_waitcnt(kWaitVmAll);
     }
-    __builtin_amdgcn_s_waitcnt(kWaitVmAll);
     __syncthreads();
     const int tb = b0 + tile * C::KEYS + kTile * kw;  // this wave's 32 keys
     if (tb >= span.hi || tb >= b1 || tb + kTile <= span.lo) continue;  // (wave-uniform) no row sees them
@@ -310,17 +349,17 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
   }
 }
 
-template <int D>
+template <int D, bool FOUR>
 void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
   const dim3 grid(a.n_layers * s.Hkv * a.splits * a.row_blocks);
   if (rpb == 32) {
-    if constexpr (D <= 128) hipExtLaunchKernelGGL((k_attn_prefix32<D, 1, 2>), grid, dim3(128), 0, st, ev0, ev1, 0, s, a);
-    else hipExtLaunchKernelGGL((k_attn_prefix32<D, 1, 1>), grid, dim3(64), 0, st, ev0, ev1, 0, s, a);
+    if constexpr (D <= 128) hipExtLaunchKernelGGL((k_attn_prefix32<D, 1, 2, FOUR>), grid, dim3(128), 0, st, ev0, ev1, 0, s, a);
+    else hipExtLaunchKernelGGL((k_attn_prefix32<D, 1, 1, FOUR>), grid, dim3(64), 0, st, ev0, ev1, 0, s, a);
   } else if (rpb == 64) {
-    if constexpr (D <= 128) hipExtLaunchKernelGGL((k_attn_prefix32<D, 2, 2>), grid, dim3(256), 0, st, ev0, ev1, 0, s, a);
-    else hipExtLaunchKernelGGL((k_attn_prefix32<D, 2, 1>), grid, dim3(128), 0, st, ev0, ev1, 0, s, a);
+    if constexpr (D <= 128) hipExtLaunchKernelGGL((k_attn_prefix32<D, 2, 2, FOUR>), grid, dim3(256), 0, st, ev0, ev1, 0, s, a);
+    else hipExtLaunchKernelGGL((k_attn_prefix32<D, 2, 1, FOUR>), grid, dim3(128), 0, st, ev0, ev1, 0, s, a);
   } else {
-    hipExtLaunchKernelGGL((k_attn_prefix32<D, 4, 1>), grid, dim3(256), 0, st, ev0, ev1, 0, s, a);
+    hipExtLaunchKernelGGL((k_attn_prefix32<D, 4, 1, FOUR>), grid, dim3(256), 0, st, ev0, ev1, 0, s, a);
   }
 }
 
@@ -329,7 +368,11 @@ void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, h
 hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
                            hipEvent_t ev1) {
   switch (s.D) {
-#define PREFIX_CASE(DD) case DD: launch_d<DD>(s, a, rows_per_block, st, ev0, ev1); break;
+#define PREFIX_CASE(DD)                                                       \
+  case DD:                                                                    \
+    if (a.four) launch_d<DD, true>(s, a, rows_per_block, st, ev0, ev1);       \
+    else launch_d<DD, false>(s, a, rows_per_block, st, ev0, ev1);             \
+    break;
     PREFIX_CASE(32) PREFIX_CASE(64) PREFIX_CASE(96) PREFIX_CASE(128)
     PREFIX_CASE(160) PREFIX_CASE(192) PREFIX_CASE(224) PREFIX_CASE(256)
 #undef PREFIX_CASE

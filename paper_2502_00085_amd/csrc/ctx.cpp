@@ -302,7 +302,7 @@ td_status td_create(const td_desc* d, td_ctx** out) {
       (e = alloc(c, &s.token, tc)) != hipSuccess || (e = alloc(c, &s.depth, tc)) != hipSuccess ||
       (e = alloc(c, &s.mask, tc)) != hipSuccess ||
       (e = alloc(c, &s.leaf_score, (size_t)s.T * s.b)) != hipSuccess ||
-      (e = alloc(c, &s.status, 2)) != hipSuccess || (e = alloc(c, &s.prefix, 1)) != hipSuccess ||
+      (e = alloc(c, &s.status, 2)) != hipSuccess || (e = alloc(c, &s.prefix, 2)) != hipSuccess ||
       (e = alloc(c, &s.lse_part, (size_t)s.T * s.b * s.lse_chunks * 2)) != hipSuccess ||
       (e = alloc(c, &s.topk_keys, 2 * (size_t)s.T * s.b * s.lse_chunks * 16)) != hipSuccess ||
       (e = alloc(c, &s.newpos, tc)) != hipSuccess || (e = alloc(c, &s.moves, tc)) != hipSuccess ||

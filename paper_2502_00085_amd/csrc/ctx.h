@@ -23,6 +23,7 @@ struct td_ctx {
   int splits_override = 0;             // TD_ATTN_SPLITS (tuning): WGs per attention unit
   // the shared prefix (td_set_prefix): as the device header has it, and the workspaces of its passes
   bool prefix = false;                 // attached
+  bool prefix_four = false;            // in 4 bits (td_set_prefix4)
   int32_t prefix_length = 0, prefix_room = 0;
   int32_t* prefix_table = nullptr;     // device, room for prefix_table_cap entries and the padding
   size_t prefix_table_cap = 0;

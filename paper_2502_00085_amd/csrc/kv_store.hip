@@ -4,7 +4,9 @@
 // Pair i of a head's first `rotary` elements, at position p, turns by the angle p f_i:
 //   (x, y) -> (x cos - y sin, y cos + x sin),   (x, y) = elements (i, i + rotary / 2), or (2i, 2i + 1);
 // the other elements, and V, are copied.  A node's position is the prefix's length plus its depth,
-// both read here, on the device: the caller need not know where a trie has got to.
+// both read here, on the device: the caller need not know where a trie has got to.  With positions of
+// several axes (images, video) p is that of the pair's axis: given for each row, or the row's own plus a
+// shift of its trie.
 //
 // The angle of a far position needs more than fp32: p f_i in turns, in 64 bits, less whole turns;
 // the sine and cosine of the rest in fp32, once per (row, pair), in LDS for all of the row's heads.
@@ -15,71 +17,39 @@
 // angles are computed once for the 32 to 48 heads of a row.
 #include <algorithm>
 
-#include "attn_common.h"
-#include "prefix.h"
+#include "kv_rows.h"
 
 namespace td {
 
 namespace {
 
-constexpr int kStoreThreads = 256;
-constexpr int kStoreRows = 8;  // rows of a WG at most
-
-template <typename T>
-struct StoreCfg {
-  static constexpr int E = 16 / (int)sizeof(T);  // elements per 16-byte chunk
-  typedef T vec __attribute__((ext_vector_type(16 / (int)sizeof(T))));
-};
-
 // Grid (row groups, layers); a WG takes `group` consecutive rows (trie, j) of one layer.
-template <typename T>
+template <typename T, bool AXES>
 __global__ __launch_bounds__(kStoreThreads) void k_store(DevState s, StoreArgs a, int group) {
   using C = StoreCfg<T>;
   using V = typename C::vec;
   constexpr int E = C::E;
-  __shared__ float2 turn[kStoreRows * 128];  // (cos, sin) of row, pair
-  __shared__ int64_t dst[kStoreRows];        // K/V row of KV head 0, -1: none
-  __shared__ int position[kStoreRows];       // -1: no row
+  __shared__ float2 turn[kStoreRows * kStorePairs];  // (cos, sin) of row, pair
+  __shared__ int64_t dst[kStoreRows];                // K/V row of KV head 0, -1: none
+  __shared__ int position[kStoreRows];               // -1: no row
   const int tid = threadIdx.x, li = blockIdx.y, lab = a.layer_begin + li;
   const int rows = a.tries * a.n, r0 = blockIdx.x * group, count = min(group, rows - r0);
   const int pairs = a.rotary / 2;
   const bool chunk = a.rows == PrefixRows::kChunk;
-  const PrefixHdr p = *s.prefix;
+  const PrefixHdr p = s.prefix[0];
   if (tid < count) {
-    const int t = (r0 + tid) / a.n, j = (r0 + tid) % a.n;
-    int pos = -1;
-    int64_t to = -1;
-    if (chunk) {
-      // (a captured call may find a shorter table than the one it was checked against)
-      if (a.pos0 + j < p.room) {
-        pos = a.pos0 + j;
-        const int64_t page = p.table[pos >> p.shift];
-        to = (((page * s.L + lab) * s.Hkv) << p.shift) + (pos & ((1 << p.shift) - 1));
-      } else {
-        set_status(s.status, kDevEinval);
-      }
-    } else {
-      const TrieHdr h = s.hdr[t];
-      int slot;
-      if (a.rows == PrefixRows::kLeaves) slot = j < h.n_live ? h.n_nodes - h.n_live + j : -1;
-      else slot = a.qslots[(size_t)t * a.n + j];
-      if (slot >= 0 && slot < h.n_nodes) {
-        const int at = h.base + slot;
-        pos = p.length + (a.rows == PrefixRows::kLeaves ? h.leaf_depth : s.depth[(size_t)t * s.cap + at]);
-        to = (((int64_t)t * s.L + lab) * s.Hkv) * s.cap + at;
-      }
-    }
-    position[tid] = pos;
-    dst[tid] = to;
+    const StoreRow w = store_row(s, a, p, lab, r0 + tid);
+    position[tid] = w.position;
+    dst[tid] = w.dst;
   }
   __syncthreads();
   for (int i = tid; i < count * pairs; i += kStoreThreads) {
-    const int row = i / pairs, pair = i % pairs, pos = position[row];
-    double x = (double)pos * (double)a.freq[pair] * 0.15915494309189535;  // turns
+    const int row = i / pairs, pair = i % pairs;
+    double x = pair_position<AXES>(a, r0 + row, position[row], pair) * (double)a.freq[pair] * 0.15915494309189535;  // turns
     x -= rint(x);
     float sn, cs;
     sincospif((float)(2.0 * x), &sn, &cs);
-    turn[row * 128 + pair] = make_float2(cs, sn);
+    turn[row * kStorePairs + pair] = make_float2(cs, sn);
   }
   __syncthreads();
 
@@ -115,46 +85,28 @@ __global__ __launch_bounds__(kStoreThreads) void k_store(DevState s, StoreArgs a
       rotate = rotate && !is_v;
     }
     if (!some) continue;
-    const bool split = rotate && !a.interleaved;
-    const int c0 = split ? w : 2 * w, c1 = split ? w + turned : 2 * w + 1;
-    const V x = reinterpret_cast<const V*>(src)[c0], y = reinterpret_cast<const V*>(src)[c1];
-    V x1 = x, y1 = y;
-    if (rotate) {
-      const float2* cs = turn + row * 128 + w * E;
-      if (split) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float2 f = cs[e];
-          const float xe = (float)x[e], ye = (float)y[e];
-          x1[e] = (T)(xe * f.x - ye * f.y);
-          y1[e] = (T)(ye * f.x + xe * f.y);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          const float2 f = cs[e / 2], g = cs[E / 2 + e / 2];
-          const float xa = (float)x[e], xb = (float)x[e + 1], ya = (float)y[e], yb = (float)y[e + 1];
-          x1[e] = (T)(xa * f.x - xb * f.y);
-          x1[e + 1] = (T)(xb * f.x + xa * f.y);
-          y1[e] = (T)(ya * g.x - yb * g.y);
-          y1[e + 1] = (T)(yb * g.x + ya * g.y);
-        }
-      }
-    }
-    reinterpret_cast<V*>(out)[c0] = x1;
-    reinterpret_cast<V*>(out)[c1] = y1;
+    store_unit(src, out, w, turned, rotate, a.interleaved, [&](int pair) { return turn[row * kStorePairs + pair]; });
   }
 }
 
 }  // namespace
 
+int store_group(long rows, int n_layers) {
+  // (as many rows per WG as leave a few WGs per CU)
+  return (int)std::max(1l, std::min<long>(kStoreRows, rows * n_layers / 1024));
+}
+
 hipError_t launch_store(const DevState& s, const StoreArgs& a, hipStream_t st) {
   const long rows = (long)a.tries * a.n;
-  // (as many rows per WG as leave a few WGs per CU)
-  int group = (int)std::max(1l, std::min<long>(kStoreRows, rows * a.n_layers / 1024));
+  const int group = store_group(rows, a.n_layers);
   const dim3 grid((rows + group - 1) / group, a.n_layers);
-  if (s.dtype == TD_F32) hipLaunchKernelGGL(k_store<float>, grid, dim3(kStoreThreads), 0, st, s, a, group);
-  else hipLaunchKernelGGL(k_store<__bf16>, grid, dim3(kStoreThreads), 0, st, s, a, group);
+#define LAUNCH_STORE(T, AXES) hipLaunchKernelGGL((k_store<T, AXES>), grid, dim3(kStoreThreads), 0, st, s, a, group)
+  const bool f32 = s.dtype == TD_F32;
+  if (a.n_axes > 0 && f32) LAUNCH_STORE(float, true);
+  else if (a.n_axes > 0) LAUNCH_STORE(__bf16, true);
+  else if (f32) LAUNCH_STORE(float, false);
+  else LAUNCH_STORE(__bf16, false);
+#undef LAUNCH_STORE
   return hipGetLastError();
 }
 

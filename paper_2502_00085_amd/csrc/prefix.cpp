@@ -39,8 +39,27 @@ td_status other_device(td_ctx* c) {
   return TD_OK;
 }
 
-// The arguments that the two stores share.
-td_status store_args(td_ctx* c, const td_rope* rope, const void* q, int64_t qs, const void* k, int64_t ks, const void* v,
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Positions of several axes (null: of one).
+td_status axes_args(td_ctx* c, const td_rope_axes* x, td::StoreArgs* a) {
+  if (!x) return TD_OK;
+  if (x->n_axes < 1 || x->n_axes > 4) return fail(c, TD_EINVAL, "rope axes: n_axes must be in [1, 4]");
+  if (!x->h_axis) return fail(c, TD_EINVAL, "rope axes: h_axis must be non-null");
+  for (int i = 0; i < x->rope.dim / 2; ++i) {
+    if (x->h_axis[i] >= x->n_axes) return fail(c, TD_EINVAL, "rope axes: pair %d has axis %d of %d", i, x->h_axis[i], x->n_axes);
+    a->axis[i / 32] |= (uint64_t)x->h_axis[i] << (2 * (i % 32));
+  }
+  if (x->d_pos && x->d_shift) return fail(c, TD_EINVAL, "rope axes: pass d_pos or d_shift, not both");
+  if (!aligned4(x->d_pos) || !aligned4(x->d_shift)) return fail(c, TD_EINVAL, "rope axes: d_pos and d_shift must be 4-byte aligned");
+  a->n_axes = x->n_axes;
+  a->positions = x->d_pos;
+  a->shift = x->d_shift;
+  return TD_OK;
+}
+
+// The arguments that the stores share; a rotation of several axes takes the place of `rope`.
+td_status store_args(td_ctx* c, const td_rope* rope, const td_rope_axes* axes, const void* q, int64_t qs, const void* k, int64_t ks, const void* v,
                      int64_t vs, void* q_out, td::StoreArgs* a) {
   const td::DevState& s = c->dev;
   if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (v == nullptr) || (!q && !k))
@@ -54,6 +73,7 @@ td_status store_args(td_ctx* c, const td_rope* rope, const void* q, int64_t qs, 
   if (a->q_stride < qr || a->k_stride < kr || a->v_stride < kr || a->q_stride % 8 || a->k_stride % 8 || a->v_stride % 8)
     return fail(c, TD_EINVAL, "row strides must be at least heads * head_dim and multiples of 8");
   if (q && q == q_out && a->q_stride != qr) return fail(c, TD_EINVAL, "q_out may be q only where q is contiguous");
+  if (axes) rope = &axes->rope;
   if (rope) {
     if (!rope->d_freq || rope->dim < 16 || rope->dim > s.D || rope->dim % 16)
       return fail(c, TD_EINVAL, "rope: d_freq must be non-null and dim a multiple of 16 in [16, head_dim]");
@@ -62,6 +82,7 @@ td_status store_args(td_ctx* c, const td_rope* rope, const void* q, int64_t qs, 
     a->rotary = rope->dim;
     a->interleaved = rope->interleaved;
   }
+  if (td_status r = axes_args(c, axes, a)) return r;
   a->q = q;
   a->k = k;
   a->v = v;
@@ -95,6 +116,7 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   a.row_blocks = (int)((rows + rpb - 1) / rpb);
   const long keys = s.W > 0 ? std::min(c->prefix_length, s.W) : c->prefix_length;
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * s.T * qn * s.Hq));
+  a.four = c->prefix_four;
   a.splits = prefix_splits(s, (long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
   a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
   a.records = a.splits;
@@ -156,13 +178,15 @@ hipError_t prefix_merge(td_ctx* c, bool nodes, const AttnArgs& a, int splits, in
 
 extern "C" {
 
-static td_status set_prefix(td_ctx* c, const td_prefix* d) {
+// Attaches d's pages, whose scales d4 has where they are in 4 bits (d null: detaches).
+static td_status set_prefix(td_ctx* c, const td_prefix* d, const td_prefix4* d4) {
   const td::DevState& s = c->dev;
-  td::PrefixHdr h;
+  td::PrefixHdr h, off;
   std::vector<int32_t> table;
   if (d) {
     if (!d->k_pages || !d->v_pages || !aligned16(d->k_pages) || !aligned16(d->v_pages))
       return fail(c, TD_EINVAL, "k_pages / v_pages must be non-null and 16-byte aligned");
+    if (d4 && (!d4->k_scales || !d4->v_scales)) return fail(c, TD_EINVAL, "k_scales / v_scales must be non-null");
     if (d->n_pages < 1 || !d->h_page_table || d->n_table < 1 || d->n_table > d->n_pages)
       return fail(c, TD_EINVAL, "need n_pages >= 1 and a page table of 1 .. n_pages entries");
     if (d->page_size < 16 || d->page_size > 65536 || (d->page_size & (d->page_size - 1)))
@@ -181,9 +205,14 @@ static td_status set_prefix(td_ctx* c, const td_prefix* d) {
     table.insert(table.end(), td::kPrefixTablePad, table[0]);
     h.k = d->k_pages;
     h.v = d->v_pages;
-    h.length = d->length;
+    h.length = h.offset = off.offset = d->length;
     h.room = (int32_t)room;
     while ((1 << h.shift) < d->page_size) ++h.shift;
+    off.other = 1;
+  }
+  if (d4) {
+    h.k_scale = static_cast<const uint8_t*>(d4->k_scales);
+    h.v_scale = static_cast<const uint8_t*>(d4->v_scales);
   }
   if (td_status r = other_device(c)) return r;
   hipError_t e = hipDeviceSynchronize();
@@ -208,35 +237,50 @@ static td_status set_prefix(td_ctx* c, const td_prefix* d) {
     if (e == hipSuccess) e = hipMemcpy(c->prefix_table, table.data(), table.size() * 4, hipMemcpyHostToDevice);
     h.table = c->prefix_table;
   }
-  if (e == hipSuccess) e = hipMemcpy(s.prefix, &h, sizeof h, hipMemcpyHostToDevice);
-  if (e != hipSuccess) return hip_fail(c, e, "td_set_prefix");
+  const td::PrefixHdr both[2] = {d4 ? off : h, d4 ? h : off};
+  if (e == hipSuccess) e = hipMemcpy(s.prefix, both, sizeof both, hipMemcpyHostToDevice);
+  if (e != hipSuccess) return hip_fail(c, e, d4 ? "td_set_prefix4" : "td_set_prefix");
   c->prefix = d != nullptr;
+  c->prefix_four = d4 != nullptr;
   c->prefix_length = h.length;
   c->prefix_room = h.room;
   return TD_OK;
 }
 
-td_status td_set_prefix(td_ctx* c, const td_prefix* d) {
+static td_status attach(td_ctx* c, const td_prefix* d, const td_prefix4* d4) {
   if (!c) return TD_EINVAL;
   c->err.clear();
   try {
-    return set_prefix(c, d);
+    return set_prefix(c, d, d4);
   } catch (const std::bad_alloc&) {  // (the table's copy)
     return fail(c, TD_EINVAL, "out of host memory for the page table");
   }
 }
 
-td_status trie_prefix_store(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n, const td_rope* rope,
-                            const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v,
-                            int64_t v_stride, void* d_q_out, hipStream_t st) {
+td_status td_set_prefix(td_ctx* c, const td_prefix* d) { return attach(c, d, nullptr); }
+
+td_status td_set_prefix4(td_ctx* c, const td_prefix4* d) {
+  if (!d) return attach(c, nullptr, nullptr);
+  const td_prefix p = {d->k_pages, d->v_pages, d->n_pages, d->page_size, d->h_page_table, d->n_table, d->length};
+  return attach(c, &p, d);
+}
+
+static td_status prefix_room(td_ctx* c, int32_t pos, int32_t n) {
+  if (!c->prefix) return fail(c, TD_ESTATE, "no prefix is attached (td_set_prefix)");
+  if (n < 1 || pos < 0 || n > c->prefix_room || pos > c->prefix_room - n)
+    return fail(c, TD_EINVAL, "positions [%d, +%d) outside the prefix's %d", pos, n, c->prefix_room);
+  return TD_OK;
+}
+
+static td_status prefix_store(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n, const td_rope* rope,
+                              const td_rope_axes* axes, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
+                              const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t st) {
   if (!c) return TD_EINVAL;
   c->err.clear();
   if (td_status r = bad_layers(c, layer_begin, n_layers)) return r;
   td::StoreArgs a{};
-  if (td_status r = store_args(c, rope, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, &a)) return r;
-  if (!c->prefix) return fail(c, TD_ESTATE, "no prefix is attached (td_set_prefix)");
-  if (n < 1 || pos < 0 || n > c->prefix_room || pos > c->prefix_room - n)
-    return fail(c, TD_EINVAL, "positions [%d, +%d) outside the prefix's %d", pos, n, c->prefix_room);
+  if (td_status r = store_args(c, rope, axes, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, &a)) return r;
+  if (td_status r = prefix_room(c, pos, n)) return r;
   if (n > kStoreRows) return fail(c, TD_EINVAL, "n must be at most 2^26");
   if (td_status r = other_device(c)) return r;
   a.rows = td::PrefixRows::kChunk;
@@ -245,14 +289,48 @@ td_status trie_prefix_store(td_ctx* c, int32_t layer_begin, int32_t n_layers, in
   a.tries = 1;
   a.n = n;
   a.pos0 = pos;
-  const hipError_t e = td::launch_store(c->dev, a, st);
+  const hipError_t e = c->prefix_four ? td::launch_store4(c->dev, a, st) : td::launch_store(c->dev, a, st);
   if (e != hipSuccess) return hip_fail(c, e, "trie_prefix_store launch");
   return TD_OK;
 }
 
-td_status trie_store_kv(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t q_max, const int32_t* d_qslots,
-                        const td_rope* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
-                        const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t st) {
+td_status trie_prefix_store(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n, const td_rope* rope,
+                            const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v,
+                            int64_t v_stride, void* d_q_out, hipStream_t st) {
+  return prefix_store(c, layer_begin, n_layers, pos, n, rope, nullptr, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, st);
+}
+
+td_status trie_prefix_store_axes(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n,
+                                 const td_rope_axes* rope, const void* d_q, int64_t q_stride, const void* d_k,
+                                 int64_t k_stride, const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t st) {
+  return prefix_store(c, layer_begin, n_layers, pos, n, nullptr, rope, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, st);
+}
+
+td_status trie_prefix_load(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n, void* d_k, void* d_v,
+                           hipStream_t st) {
+  if (!c) return TD_EINVAL;
+  c->err.clear();
+  if (td_status r = bad_layers(c, layer_begin, n_layers)) return r;
+  if ((!d_k && !d_v) || !aligned16(d_k) || !aligned16(d_v)) return fail(c, TD_EINVAL, "pass k or v, or both, 16-byte aligned");
+  if (td_status r = prefix_room(c, pos, n)) return r;
+  if (n > kStoreRows) return fail(c, TD_EINVAL, "n must be at most 2^26");
+  if (td_status r = other_device(c)) return r;
+  td::LoadArgs a{};
+  a.k = d_k;
+  a.v = d_v;
+  a.layer_begin = layer_begin;
+  a.n_layers = n_layers;
+  a.pos0 = pos;
+  a.n = n;
+  a.four = c->prefix_four;
+  const hipError_t e = td::launch_prefix_load(c->dev, a, st);
+  if (e != hipSuccess) return hip_fail(c, e, "trie_prefix_load launch");
+  return TD_OK;
+}
+
+static td_status store_kv(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t q_max, const int32_t* d_qslots,
+                          const td_rope* rope, const td_rope_axes* axes, const void* d_q, int64_t q_stride, const void* d_k,
+                          int64_t k_stride, const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t st) {
   td_status r = td::check_ready(c);
   if (r != TD_OK) return r;
   const td::DevState& s = c->dev;
@@ -260,7 +338,7 @@ td_status trie_store_kv(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_
   if (d_qslots ? q_max < 1 : q_max != s.b) return fail(c, TD_EINVAL, "q_max must be >= 1, or the beam width for the leaves");
   if ((int64_t)s.T * q_max > kStoreRows) return fail(c, TD_EINVAL, "n_tries * q_max must be at most 2^26");
   td::StoreArgs a{};
-  if ((r = store_args(c, rope, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, &a)) != TD_OK) return r;
+  if ((r = store_args(c, rope, axes, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, &a)) != TD_OK) return r;
   if (d_qslots && c->pending) return fail(c, TD_ESTATE, "the leaves' K/V are pending: store them first");
   if ((r = other_device(c)) != TD_OK) return r;
   a.rows = d_qslots ? td::PrefixRows::kNodes : td::PrefixRows::kLeaves;
@@ -277,6 +355,18 @@ td_status trie_store_kv(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_
   return TD_OK;
 }
 
+td_status trie_store_kv(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t q_max, const int32_t* d_qslots,
+                        const td_rope* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
+                        const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t st) {
+  return store_kv(c, layer_begin, n_layers, q_max, d_qslots, rope, nullptr, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, st);
+}
+
+td_status trie_store_kv_axes(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t q_max, const int32_t* d_qslots,
+                             const td_rope_axes* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
+                             const void* d_v, int64_t v_stride, void* d_q_out, hipStream_t st) {
+  return store_kv(c, layer_begin, n_layers, q_max, d_qslots, nullptr, rope, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, st);
+}
+
 td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n, const void* d_q,
                            void* d_out, float scale, hipStream_t st) {
   if (!c) return TD_EINVAL;
@@ -286,9 +376,7 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
   if (!d_q || !d_out || !aligned16(d_q) || !aligned16(d_out))
     return fail(c, TD_EINVAL, "q / out must be non-null and 16-byte aligned");
   if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(c, TD_EINVAL, "scale must be finite and > 0");
-  if (!c->prefix) return fail(c, TD_ESTATE, "no prefix is attached (td_set_prefix)");
-  if (n < 1 || pos < 0 || n > c->prefix_room || pos > c->prefix_room - n)
-    return fail(c, TD_EINVAL, "positions [%d, +%d) outside the prefix's %d", pos, n, c->prefix_room);
+  if (td_status r = prefix_room(c, pos, n)) return r;
   const int G = s.Hq / s.Hkv;
   if ((int64_t)n * G > (1 << 24)) return fail(c, TD_EINVAL, "n must be at most 2^24 / (Hq / Hkv)");
   if (td_status r = other_device(c)) return r;
@@ -305,6 +393,7 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
     a.q = static_cast<const char*>(d_q) + l * layer;
     a.out = static_cast<char*>(d_out) + l * layer;
     a.rows = td::PrefixRows::kChunk;
+    a.four = c->prefix_four;
     a.layer_begin = layer_begin + l;
     a.n_layers = std::min(lc, n_layers - l);
     a.tries = 1;

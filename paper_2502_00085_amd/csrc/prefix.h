@@ -29,6 +29,7 @@ struct PrefixArgs {
   int records = 1;                  // per row: splits, and after them trie_splits
   int xcd_group = 0;                // row blocks of one (layer, KV head, split) on one XCD
   int pair_blocks = 0;              // (with it, kChunk) an XCD's WGs in an order that evens out its CUs
+  int four = 0;                     // the prefix is the one in 4 bits
   // (kLeaves, bf16) the same launch takes the tries' own nodes too, all of which are stored: after
   // prefix_wgs WGs come those of (layer, trie, KV head, block of a trie's rows, split of its nodes)
   int trie_splits = 0, trie_blocks = 0;
@@ -68,7 +69,23 @@ struct StoreArgs {
   int pos0;                 // (kChunk)
   int rotary, interleaved;
   int64_t q_stride, k_stride, v_stride;  // elements from one row to the next
+  // positions of several axes (n_axes > 0): of each row and axis, or (null) the row's own plus shift
+  int n_axes = 0;
+  uint64_t axis[4] = {};    // of pair i: bits 2 (i % 32) .. of word i / 32
+  const int32_t* positions = nullptr;  // [tries][n][n_axes]
+  const int32_t* shift = nullptr;      // [tries][n_axes], null: none
 };
 hipError_t launch_store(const DevState& s, const StoreArgs& a, hipStream_t st);
+hipError_t launch_store4(const DevState& s, const StoreArgs& a, hipStream_t st);
+
+// Rows of the prefix back: positions pos0 .. pos0 + n - 1, [n_layers][n][Hkv][D] of the context's type.
+struct LoadArgs {
+  void *k, *v;              // either may be null
+  int layer_begin, n_layers, pos0, n;
+  int four = 0;
+};
+hipError_t launch_prefix_load(const DevState& s, const LoadArgs& a, hipStream_t st);
+// Rows that one workgroup of a store or load takes.
+int store_group(long rows, int n_layers);
 
 }  // namespace td

@@ -27,17 +27,24 @@ struct alignas(16) TrieHdr {
 };
 static_assert(sizeof(TrieHdr) == 64, "one 64-byte header per trie");
 
-// The shared prefix as the kernels see it (one per context, in device memory: a captured call reads
-// the prefix that is attached when it is replayed).
+// The shared prefix as the kernels see it (in device memory: a captured call reads the prefix that is
+// attached when it is replayed).  A context has two, [0] of pages in its own type and [1] of 4-bit pages;
+// the one that is not attached has no position and no room, so that a captured call of the other kind
+// finds nothing to read.
 struct alignas(16) PrefixHdr {
-  const void* k = nullptr;         // [n_pages][L][Hkv][2^shift][D]
+  const void* k = nullptr;         // [n_pages][L][Hkv][2^shift][D], or [..][D / 2] bytes in 4 bits
   const void* v = nullptr;
   const int32_t* table = nullptr;  // page of positions i 2^shift ..; padded by kPrefixTablePad entries
   int32_t length = 0;              // positions that the tries attend to
   int32_t shift = 0;               // log2 of the page size
   int32_t room = 0;                // positions that the table has pages for
-  int32_t pad = 0;
+  int32_t offset = 0;              // position of a node of depth 0 (both headers: the attached one's length)
+  const uint8_t* k_scale = nullptr;  // (4 bits) [n_pages][L][Hkv][2^shift][D / 32]
+  const uint8_t* v_scale = nullptr;
+  int32_t other = 0;               // 1: a prefix of the other kind is attached
+  int32_t pad[3] = {0, 0, 0};
 };
+static_assert(sizeof(PrefixHdr) == 80, "two headers, read by scalar loads");
 constexpr int kPrefixTablePad = 8;
 
 // Device-side pointers of one context.  Node arrays are [T][cap], indexed by physical slot.
@@ -75,7 +82,7 @@ struct DevState {
   int32_t* n_moves;      // [T]
   float* attn_part;      // split-combine partials
   int lse_chunks, attn_part_floats, attn_pairs_max;
-  PrefixHdr* prefix = nullptr;  // (contexts of tries; no prefix attached: zeros)
+  PrefixHdr* prefix = nullptr;  // [2] (contexts of tries; no prefix attached: zeros)
 };
 
 // Batch-based beam search baseline (Alg 1): state of the cache reorder.  `req` holds one
