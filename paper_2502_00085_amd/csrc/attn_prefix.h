@@ -134,6 +134,13 @@ __device__ inline TilePages tile_pages(const PrefixHdr& h, int tile) {
 // after row, are numbers 0 .. KEYS D / 32 - 1, its V blocks follow, and thread tid holds blocks j THREADS +
 // tid (of K or of V alike in a wave, unless KEYS D / 32 is no multiple of 64).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// (pointers into global memory: a load through a pointer that was itself loaded would be a flat one, whose
+// arrival only a wait for all of them tells)
+typedef const __attribute__((address_space(1))) unsigned char* global_bytes;
+typedef const __attribute__((address_space(1))) u32x4* global_u32x4;
+typedef const __attribute__((address_space(1))) u32x2* global_u32x2;
+__device__ inline global_bytes to_global(const void* p) { return (global_bytes)(uintptr_t)p; }
 template <int D, int THREADS, int KEYS>
 struct Blocks4 {
   static constexpr int BPR = D / 32;         // blocks per row
@@ -159,25 +166,23 @@ __device__ inline void fetch4(const PrefixHdr& p, const TilePages& pg, size_t pa
   const bool one = p.shift >= 6, whole = one && last >= KEYS - 1;  // (uniform)
   const size_t row0 = (size_t)pg.p[0] * page_rows + head + (one ? tb & ((1 << p.shift) - 1) : 0);
   // (copies: a choice between members would keep the header in scratch memory)
-  const unsigned char *kx = static_cast<const unsigned char*>(p.k), *vx = static_cast<const unsigned char*>(p.v);
-  const uint8_t *ksc = p.k_scale, *vsc = p.v_scale;
+  const global_bytes kx = to_global(p.k), vx = to_global(p.v), ksc = to_global(p.k_scale), vsc = to_global(p.v_scale);
   const int p0 = pg.p[0], p1 = pg.p[1], p2 = pg.p[2], p3 = pg.p[3];
 #pragma unroll
   for (int j = 0; j < B::PER; ++j) {
     if (!B::some(j, wave)) continue;
     const bool v = B::is_v(j, wave);
-    const unsigned char* x = v ? vx : kx;
-    const uint8_t* sc = v ? vsc : ksc;
+    const global_bytes x = v ? vx : kx, sc = v ? vsc : ksc;
     const uint32_t b = B::number(j, v);
     if (whole) {
-      to.x[j] = *reinterpret_cast<const u32x4*>(x + row0 * (D / 2) + b * 16);
+      to.x[j] = *(global_u32x4)(x + row0 * (D / 2) + b * 16);
       to.scale[j] = (sc + row0 * B::BPR)[b];
     } else {
       const int row = min((int)(b / B::BPR), last), n = (tb & 63) + row;
       const int e = one ? 0 : n >> p.shift;
       const int page = e == 0 ? p0 : e == 1 ? p1 : e == 2 ? p2 : p3;
       const size_t at = one ? row0 + row : (size_t)page * page_rows + head + (n & ((1 << p.shift) - 1));
-      to.x[j] = *reinterpret_cast<const u32x4*>(x + at * (D / 2) + b % B::BPR * 16);
+      to.x[j] = *(global_u32x4)(x + at * (D / 2) + b % B::BPR * 16);
       to.scale[j] = sc[at * B::BPR + b % B::BPR];
     }
   }

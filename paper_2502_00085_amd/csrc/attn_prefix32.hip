@@ -194,6 +194,8 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
   auto vat = [&](int dt, int v) __attribute__((always_inline)) {  // key 8 (v / 4) + 4 hh + v % 4, element 32 dt + col
     return *reinterpret_cast<const float*>(vrow + (8 * (v >> 2) + (v & 3)) * (D * 4) + voff[dt]);
   };
+  // (the queries are there: else each tile's products would wait for them, and so for the tile under way)
+  if constexpr (FOUR) __builtin_amdgcn_s_waitcnt(kWaitVmAll);
 #pragma unroll 1
   for (int tile = 0; tile < n_tiles; ++tile) {
     if constexpr (FOUR) {

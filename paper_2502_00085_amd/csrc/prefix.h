@@ -44,6 +44,9 @@ hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st,
 hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
                            hipEvent_t ev1);
 
+hipError_t launch_prefix4(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
+                          hipEvent_t ev1);
+
 // Merges a pass's records with those of the tries (attention partials of `splits` splits in blocks of
 // block_rows rows, null: none) into out [n_layers][tries][per_trie][Hq][D].
 struct PrefixMergeArgs {

@@ -307,7 +307,7 @@ def test_graph_reads_the_attached_prefix():
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_kinds_in_turn(dtype):
     """Prefixes of both kinds, attached one after the other to one context: each as if it were the only one.  The
-    plain one holds what the 4-bit one stands for: the same outputs."""
+    plain one holds what the 4-bit one stands for: the same outputs but for the order of sums."""
     dt = plain.DT[dtype]
     bt = Batch(dtype, 64, 4, 2, 300, 32, [(20, 3), (35, 2)], 4, L=2)
     same = Prefix(bt.gen, bt.rng, 2, 2, 64, dt, 300, 16)
@@ -325,8 +325,10 @@ def test_kinds_in_turn(dtype):
             bt.prefix.attach(bt.dec)
         outs.append(torch.full_like(q, 9.0))
         bt.dec.attn_decode(0, 2, q, None, None, outs[-1], bt.scale)
-    for o in outs[1:]:
-        assert torch.equal(o, outs[0])
+    assert torch.equal(outs[2], outs[0]) and torch.equal(outs[3], outs[1])
+    # (the same sums in another order: two roundings of either output and of its weights)
+    h = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -16
+    assert float((outs[1].float() - outs[0].float()).abs().max()) <= 4 * h * float(outs[0].float().abs().max())
     bt.prefix.attach(bt.dec)
     bt.decode()
 
