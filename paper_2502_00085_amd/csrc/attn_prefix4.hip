@@ -33,7 +33,6 @@ constexpr int kFewWaves = 4;
 
 template <int D>
 struct FewCfg {
-  static constexpr int THREADS = 64 * kFewWaves;
   static constexpr int KSTEPS = D / 16;  // 32x32x16 steps of S^T: 8 elements of a lane's half row
   static constexpr int DT = D / 32;
   static constexpr int CPR = D / 8;
@@ -309,7 +308,7 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
     if (i + 1 < mine) step(std::true_type{}, i + 1, k1, v1);
   }
 
-  // the four waves' states become one, two and two: O goes through LDS lane by lane
+  // the waves' states become one, two and two: O goes through LDS lane by lane
   static_assert(64 * (D / 2) * 4 == 2 * C::VBUF, "a wave's O takes two waves' V rows");
 #pragma unroll
   for (int half = kFewWaves / 2; half >= 1; half >>= 1) {
@@ -344,17 +343,17 @@ __global__ __launch_bounds__(64 * kFewWaves, FewCfg<D>::WAVES) void k_attn_prefi
   few_wg<D>(s, a, vbuf, ml);
 }
 
-// The same, and after prefix_wgs WGs those of the tries' own nodes, 64 rows each (half of them rows).
+// The same, and after prefix_wgs WGs those of the tries' own nodes, 64 rows each (32 of them rows).
 template <int D>
 __global__ __launch_bounds__(64 * kFewWaves, FewCfg<D>::WAVES) void k_attn_prefix4_few_tries(DevState s, PrefixArgs a) {
   using C = PrefixCfg<D, 2, 2>;
-  static_assert(C::THREADS == 64 * kFewWaves && 2 * C::BUF >= kFewWaves * FewCfg<D>::VBUF, "the same WG");
-  __shared__ __attribute__((aligned(16))) unsigned char kbuf0[2][C::BUF];
+  static_assert(C::THREADS == 64 * kFewWaves && 2 * C::BUF == kFewWaves * FewCfg<D>::VBUF, "the same WG");
+  __shared__ __attribute__((aligned(16))) unsigned char buf[2][C::BUF];
   __shared__ __attribute__((aligned(16))) unsigned char kbuf1[C::BUF], vbuf1[C::BUF];
   __shared__ int wred[8];
   __shared__ float ml[256];
-  if (blockIdx.x >= a.prefix_wgs) prefix_wg<D, 2, 2, Wgs::kTries, false>(s, a, kbuf0[0], kbuf0[1], kbuf1, vbuf1, wred, ml);
-  else few_wg<D>(s, a, kbuf0[0], ml);
+  if (blockIdx.x >= a.prefix_wgs) prefix_wg<D, 2, 2, Wgs::kTries, false>(s, a, buf[0], buf[1], kbuf1, vbuf1, wred, ml);
+  else few_wg<D>(s, a, buf[0], ml);
 }
 
 template <int D>

@@ -112,12 +112,12 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   a.q_stride = q_max;
   a.scale_log2 = scale_log2;
   const long rows = (long)s.T * qn * (s.Hq / s.Hkv);
-  const int rpb = prefix_rows_per_block(rows);
+  const int rpb = prefix_rows_per_block(s, c->prefix_four, rows);
   a.row_blocks = (int)((rows + rpb - 1) / rpb);
   const long keys = s.W > 0 ? std::min(c->prefix_length, s.W) : c->prefix_length;
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * s.T * qn * s.Hq));
   a.four = c->prefix_four;
-  a.splits = prefix_splits(s, (long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
+  a.splits = prefix_splits(s, a.four && rpb == 32, (long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
   a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
   a.records = a.splits;
   *tries = false;
@@ -129,13 +129,14 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
     // positions 22.1 us a layer against 30.3), at worst 4 % more (2 x 32 of 229 over 64: 21.9, 21.1).  Past
     // kTrieTiles, 11 % less to 12 % more.  The other two limits keep away from what was not measured, calls of
     // many layers, and cost one-layer calls past them 7 % (2 x 4 beams of 404 nodes over 50,000 positions, 32 KV
-    // heads, 49 tiles of the prefix per WG: 117.8, 127.2).
+    // heads, 49 tiles of the prefix per WG: 117.8, 127.2).  In 4 bits the pass may be long: 8 rows of 32 KV heads
+    // over 30,000 positions 38.9 us in one launch of 8 or 12 splits, 42.7 in two of 16.
     // A trie's WG has 3 of its tiles, which take about as long as the 4 that a WG of the prefix has at least:
     // over 160 of these shapes 1 or 2 took 1.4 % less in the mean, 4 took 4 % more, 6 8 %, 8 13 %.
     const long wgs = (long)n_layers * s.Hkv * a.row_blocks * a.splits, tiles = (trie_nodes + 63) / 64;
     const long blocks = (qn * (s.Hq / s.Hkv) + rpb - 1) / rpb, units = (long)n_layers * s.T * s.Hkv * blocks;
     const long ts = std::max(1l, std::min({(tiles + 2) / 3, 256 / units, fit - a.splits}));
-    if (wgs + units * ts <= kOneRound && (keys + 63) / 64 <= (long)kShortPass * a.splits && (tiles + ts - 1) / ts <= kTrieTiles && a.splits + ts <= fit) {
+    if (wgs + units * ts <= kOneRound && (a.four || (keys + 63) / 64 <= (long)kShortPass * a.splits) && (tiles + ts - 1) / ts <= kTrieTiles && a.splits + ts <= fit) {
       a.trie_splits = (int)ts;
       a.trie_blocks = (int)blocks;
       a.prefix_wgs = (uint32_t)wgs;
@@ -381,7 +382,7 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
   if ((int64_t)n * G > (1 << 24)) return fail(c, TD_EINVAL, "n must be at most 2^24 / (Hq / Hkv)");
   if (td_status r = other_device(c)) return r;
   const long rows = (long)n * G;
-  const int rpb = td::prefix_rows_per_block(rows), blocks = (int)((rows + rpb - 1) / rpb);
+  const int rpb = td::prefix_rows_per_block(s, c->prefix_four, rows), blocks = (int)((rows + rpb - 1) / rpb);
   // (as many layers per launch as its grid holds)
   const int lc = (int)std::max(1l, std::min<long>(n_layers, (1l << 22) / ((long)s.Hkv * blocks)));
   const size_t layer = (size_t)n * s.Hq * s.D * (s.dtype == TD_F32 ? 4 : 2);
@@ -403,7 +404,7 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
     a.row_blocks = blocks;
     const long keys = s.W > 0 ? std::min(pos + n, s.W) : pos + n, units = (long)a.n_layers * s.Hkv * blocks;
     const long fit = (long)(c->prefix_records / ((size_t)a.n_layers * n * s.Hq));
-    a.records = a.splits = td::prefix_splits(s, units, keys, std::max(1l, fit));
+    a.records = a.splits = td::prefix_splits(s, a.four && rpb == 32, units, keys, std::max(1l, fit));
     a.xcd_group = blocks > 1 && ((long)a.n_layers * s.Hkv * a.splits) % 8 == 0;
     // Two WGs per CU at once, and no third: a long block beside a short one.  2,048 tokens of 32 heads (8
     // KV heads, d = 128) from position 0: 57.5 -> 53.7 us a layer, from 6,144: 254 -> 247.5 (graphs in turn);
