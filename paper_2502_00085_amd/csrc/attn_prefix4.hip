@@ -299,11 +299,12 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
   // (the queries and the first tiles are there: else the loop would wait for the queries, and with them for
   // every load, each time it multiplies)
   __builtin_amdgcn_s_waitcnt(kWaitVmAll);
-  for (int i = 0; i < 2 * pairs; i += 2) {
+  const bool empty = span.hi == 0;  // (no row is a query's, or sees a key)
+  for (int i = empty ? 2 * pairs : 0; i < 2 * pairs; i += 2) {
     step(std::false_type{}, i, k0, v0);
     step(std::false_type{}, i + 1, k1, v1);
   }
-  for (int i = 2 * pairs; i < mine; i += 2) {
+  for (int i = empty ? mine : 2 * pairs; i < mine; i += 2) {
     step(std::true_type{}, i, k0, v0);
     if (i + 1 < mine) step(std::true_type{}, i + 1, k1, v1);
   }

@@ -281,6 +281,21 @@ __device__ __attribute__((always_inline)) inline void prefix_wg(
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[dt][v] = 0.0f;
 
+  // (4 bits) no row of the WG is a query's: its records say so, and nothing is multiplied.  4 ragged prompts of up
+  // to 512 tokens over 4,096 positions, 2 layers: 337 -> 326 us.
+  if (four && known && a.rows == PrefixRows::kNodes) {
+    if (lane == 0) wred[wave] = span.hi;
+    __syncthreads();
+    int most = 0;
+#pragma unroll
+    for (int i = 0; i < RW * KW; ++i) most = max(most, wred[i]);
+    if (__builtin_amdgcn_readfirstlane(most) == 0) {
+      unsigned char* const mine = rw == 0 ? kbuf0 : rw == 1 ? vbuf0 : rw == 2 ? kbuf1 : vbuf1;
+      if (kw == 0) prefix_output<__bf16, D>(s, a, u, q, lane, m, lsum, o, reinterpret_cast<float*>(mine));
+      return;
+    }
+  }
+
   // V^T of 16 keys and 32 elements of d: this lane's column of d = 32 dt + col
   auto vop = [&](const unsigned char* vh, int uu, int dt) __attribute__((always_inline)) {
     const unsigned char* vp = vh + 16 * uu * (2 * D);
