@@ -260,22 +260,26 @@ class RopeAxes:
             raise ValueError("axis must hold an axis in 0 .. 3 for each pair")
         self.axis = np.ascontiguousarray(axis, dtype=np.uint8)
         self.n_axes = int(axis.max()) + 1 if axis.size else 1
+        self.own = TdRopeAxes(self.rope.c, self.n_axes, self.axis.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8)), None, None)
 
     def c(self, rows: Sequence[int], tries: int, positions, shift):
         """td_rope_axes of a call whose rows have the shape ``rows``."""
-        import torch
-        for name, t, lead in (("positions", positions, rows), ("shift", shift, (tries,))):
-            if t is None:
-                continue
-            if tuple(t.shape[:-1]) != tuple(lead) or not self.n_axes <= t.shape[-1] <= 4:
-                raise ValueError(f"{name} must be {list(lead)} with {self.n_axes} to 4 axes, got {list(t.shape)}")
-            _ptr(t, torch.int32, None, name)
+        if positions is None and shift is None:
+            return self.own
         if positions is not None and shift is not None:
             raise ValueError("pass positions or shift, not both")
-        given = positions if positions is not None else shift
-        n_axes = self.n_axes if given is None else int(given.shape[-1])
-        return TdRopeAxes(self.rope.c, n_axes, self.axis.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8)),
-                          None if positions is None else positions.data_ptr(), None if shift is None else shift.data_ptr())
+        import torch
+        name, t, lead = ("shift", shift, (tries,)) if positions is None else ("positions", positions, rows)
+        shape = t.shape
+        if shape[:-1] != lead or not self.n_axes <= shape[-1] <= 4:
+            raise ValueError(f"{name} must be {list(lead)} with {self.n_axes} to 4 axes, got {list(shape)}")
+        c = TdRopeAxes.from_buffer_copy(self.own)  # (a call has its own)
+        c.n_axes = shape[-1]
+        if positions is None:
+            c.d_shift = _ptr(t, torch.int32, None, name)
+        else:
+            c.d_pos = _ptr(t, torch.int32, None, name)
+        return c
 
 
 def _rope_call(rope, rows, tries, positions, shift):

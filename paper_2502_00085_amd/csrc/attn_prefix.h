@@ -135,12 +135,8 @@ __device__ inline TilePages tile_pages(const PrefixHdr& h, int tile) {
 // tid (of K or of V alike in a wave, unless KEYS D / 32 is no multiple of 64).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-// (pointers into global memory: a load through a pointer that was itself loaded would be a flat one, whose
-// arrival only a wait for all of them tells)
-typedef const __attribute__((address_space(1))) unsigned char* global_bytes;
-typedef const __attribute__((address_space(1))) u32x4* global_u32x4;
-typedef const __attribute__((address_space(1))) u32x2* global_u32x2;
-__device__ inline global_bytes to_global(const void* p) { return (global_bytes)(uintptr_t)p; }
+typedef const TD_GLOBAL u32x4* global_u32x4;
+typedef const TD_GLOBAL u32x2* global_u32x2;
 template <int D, int THREADS, int KEYS>
 struct Blocks4 {
   static constexpr int BPR = D / 32;         // blocks per row

@@ -64,8 +64,8 @@ struct HalfRow {
     return (at < 24 ? w << (23 - at) : w >> 1) & 0x7f800000u;
   }
 };
-typedef const __attribute__((address_space(1), aligned(1))) uint16_t* global_u16;
-typedef const __attribute__((address_space(1), aligned(1))) uint32_t* global_u32;
+typedef const TD_GLOBAL uint16_t __attribute__((aligned(1))) * global_u16;
+typedef const TD_GLOBAL uint32_t __attribute__((aligned(1))) * global_u32;
 
 template <int D>
 __device__ inline void load_half(global_bytes rows, global_bytes scales, uint32_t row, int hh, HalfRow<D>& h) {

@@ -5,6 +5,12 @@
 
 namespace td {
 
+// Pointers into global memory: a load through a pointer that was itself loaded from memory would be a flat one,
+// whose arrival only a wait for all of them tells.
+#define TD_GLOBAL __attribute__((address_space(1)))
+typedef const TD_GLOBAL unsigned char* global_bytes;
+__device__ inline global_bytes to_global(const void* p) { return (global_bytes)(uintptr_t)p; }
+
 // Whose rows a prefix pass takes: the live leaves of every trie, stored nodes of every trie, or
 // consecutive positions of the prefix itself (causal).
 enum class PrefixRows { kLeaves, kNodes, kChunk };
