@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_prefix_merge(DevState s, Pref
 // 75.3; 1,024 rows 43.4 and 43.2, 125 and 119; 32 KV heads, 128 rows over 20,000 73.4 and 87; at d = 256 256 rows
 // over 20,000 99 and 69.
 int prefix_rows_per_block(const DevState& s, bool four, long rows) {
-  if (four && s.dtype == TD_BF16 && s.D <= 128 && rows <= 512) return 32;
+  if (four && s.D <= 128 && (rows <= 512 || s.dtype == TD_F32)) return 32;
   return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
 }
 
@@ -183,7 +183,7 @@ int prefix_rows_per_block(const DevState& s, bool four, long rows) {
 // KV heads, 8 rows over 30,000, 4 / 8 / 16: 60.5 / 39.3 / 42.8; 128 rows over 20,000 (313 tiles), 2 / 4: 85 / 73.4.
 int prefix_splits(const DevState& s, bool four, long units, long keys, long most) {
   const long tiles = (keys + 63) / 64;
-  if (four && s.dtype == TD_BF16 && s.D <= 128) {
+  if (four && s.D <= 128) {
     const long least = units < 16 ? 4 : 6;
     const long one = std::min(256 / units, (tiles + least - 1) / least), two = std::min(512 / units, tiles / 64);
     return (int)std::max(1l, std::min(std::max(one, two), most));
@@ -196,8 +196,8 @@ int prefix_splits(const DevState& s, bool four, long units, long keys, long most
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
   const int rpb = prefix_rows_per_block(s, a.four, (long)a.tries * a.per_trie * (s.Hq / s.Hkv));
   if (a.trie_splits > 0 && (a.rows != PrefixRows::kLeaves || s.dtype != TD_BF16 || !mfma_head_dim(s.D))) return hipErrorInvalidValue;
-  if (s.dtype == TD_F32) return launch_prefix32(s, a, rpb, st, ev0, ev1);
   if (a.four) return launch_prefix4(s, a, rpb, st, ev0, ev1);
+  if (s.dtype == TD_F32) return launch_prefix32(s, a, rpb, st, ev0, ev1);
   switch (s.D) {
 #define PREFIX_CASE(DD) case DD: launch_d<DD>(s, a, rpb, st, ev0, ev1); break;
     PREFIX_CASE(32) PREFIX_CASE(64) PREFIX_CASE(96) PREFIX_CASE(128)

@@ -106,7 +106,37 @@ __device__ inline bf16x8 half_values(const HalfRow<D>& h, int hh, int k) {
   return bf16x8{y0[0], y0[1], y1[0], y1[1], y2[0], y2[1], y3[0], y3[1]};
 }
 
-template <int D>
+// The next 8 bits of x, in bf16; x keeps the rest.  Three in a row hold all of an fp32 number.
+__device__ inline __bf16 take8(float& x) {
+  const uint32_t u = __float_as_uint(x);
+  x -= __uint_as_float(u & 0xffff0000u);
+  return __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
+}
+
+// A lane's part of a query row as bf16 operands: in bf16 itself, in fp32 three parts of it (take8).
+template <typename T, int D>
+struct FewQuery {
+  static constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+  bf16x8 x[PARTS][D / 16];
+  __device__ void load(const T* row) {
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      if constexpr (PARTS == 1) {
+        x[0][k] = reinterpret_cast<const bf16x8*>(row)[k];
+      } else {
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        const f32x4 a = reinterpret_cast<const f32x4*>(row)[2 * k], b = reinterpret_cast<const f32x4*>(row)[2 * k + 1];
+        float rest[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[i][k][e] = take8(rest[e]);
+      }
+    }
+  }
+};
+
+template <typename T, int D>
 __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, const PrefixArgs& a, unsigned char* vbuf, float* ml) {
   using C = FewCfg<D>;
   const PrefixHdr p = s.prefix[1];
@@ -117,13 +147,9 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
   const PrefixUnit u = prefix_unit(s, a);
   const int lab = a.layer_begin + u.li;
   PrefixRow q = prefix_row(s, a, u.li, u.rb * 32 + col);  // (the same 32 rows in every wave)
-  bf16x8 qv[C::KSTEPS];
-  {
-    const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const __bf16*>(a.q) +
-                                                     (q.at * s.Hq + u.g * (s.Hq / s.Hkv) + q.head) * D + hh * (D / 2));
-#pragma unroll
-    for (int k = 0; k < C::KSTEPS; ++k) qv[k] = __builtin_bit_cast(bf16x8, qp[k]);
-  }
+  constexpr int PARTS = FewQuery<T, D>::PARTS;
+  FewQuery<T, D> qv;
+  qv.load(static_cast<const T*>(a.q) + (q.at * s.Hq + u.g * (s.Hq / s.Hkv) + q.head) * D + hh * (D / 2));
   PrefixSpan span, all;
   const bool known = prefix_range(s, a, p, u.rb * 32, 32, &all);
   if (!known) {
@@ -221,7 +247,11 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
 #pragma unroll
     for (int x = 0; x < 16; ++x) acc[x] = 0.0f;
 #pragma unroll
-    for (int x = 0; x < C::KSTEPS; ++x) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(half_values<D>(k, hh, x), qv[x], acc, 0, 0, 0);
+    for (int x = 0; x < C::KSTEPS; ++x) {
+      const bf16x8 kk = half_values<D>(k, hh, x);
+#pragma unroll
+      for (int i = PARTS - 1; i >= 0; --i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qv.x[i][x], acc, 0, 0, 0);
+    }
     // (unconditional where it matters: the wait for one tile's loads counts the other's)
     if (!CUT || i + 2 < mine) {
       fetch(tile_of(i + 2), next, k, v);
@@ -235,16 +265,25 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
         acc[x] = (n >= q.lo) & (n < q.hi) ? acc[x] : -INFINITY;
       }
     }
-    // probabilities of the lane's 16 keys, as in prefix_wg: rounded to bf16, summed as rounded; the shift
-    // moves when they leave their range
-    bf16x8 pb[2];
+    // Probabilities of the lane's 16 keys, as in prefix_wg: in bf16 rounded, and summed as rounded; in fp32 in
+    // three parts, like the queries.  The shift moves when they leave their range.
+    float w[16];
+    bf16x8 pb[PARTS][2];
     float ps = 0.0f;
     auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int x = 0; x < 16; ++x) pb[x >> 3][x & 7] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(acc[x], scale, -m));
+      for (int x = 0; x < 16; ++x) w[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[x], scale, -m));
       ps = 0.0f;
+      if constexpr (PARTS == 1) {
 #pragma unroll
-      for (int x = 0; x < 16; x += 2) ps = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[x >> 3][x & 7], pb[x >> 3][(x & 7) + 1]}, ones, ps, false);
+        for (int x = 0; x < 16; ++x) pb[0][x >> 3][x & 7] = (__bf16)w[x];
+#pragma unroll
+        for (int x = 0; x < 16; x += 2)
+          ps = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pb[0][x >> 3][x & 7], pb[0][x >> 3][(x & 7) + 1]}, ones, ps, false);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) ps += w[x];
+      }
     };
     weights();
     if (__any(ps > kMost)) {
@@ -269,10 +308,10 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
 #pragma unroll 1
       for (int n = 0; n < 32; ++n) {
         const int vi = (n >> 3) * 4 + (n & 3);
-        float w = 0.0f;
+        float wn = 0.0f;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) w = x == vi ? (float)pb[x >> 3][x & 7] : w;
-        w = __shfl(w, col + 32 * ((n >> 2) & 1));
+        for (int x = 0; x < 16; ++x) wn = x == vi ? (PARTS == 1 ? (float)pb[0][x >> 3][x & 7] : w[x]) : wn;
+        wn = __shfl(wn, col + 32 * ((n >> 2) & 1));
         const bool own = tb + n >= q.lo && tb + n < q.hi;
 #pragma unroll
         for (int dt = 0; dt < C::DT; ++dt)
@@ -280,10 +319,16 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
           for (int q4 = 0; q4 < 4; ++q4) {
             const bf16x4 x = *reinterpret_cast<const bf16x4*>(vmine + n * (2 * D) + few_chunk<D>(n, 4 * dt + q4) * 16 + 8 * hh);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[dt][4 * q4 + e] += own ? w * (float)x[e] : 0.0f;
+            for (int e = 0; e < 4; ++e) o[dt][4 * q4 + e] += own ? wn * (float)x[e] : 0.0f;
           }
       }
       return;
+    }
+    if constexpr (PARTS > 1) {
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) pb[i][x >> 3][x & 7] = take8(w[x]);
     }
 #pragma unroll
     for (int uu = 0; uu < 2; ++uu)
@@ -293,7 +338,9 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
         const i16x4 p0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vp + vread[0][dt]));
         const i16x4 p1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vp + vread[1][dt]));
         const i16x8 x = __builtin_shufflevector(p0, p1, 0, 1, 2, 3, 4, 5, 6, 7);
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pb[uu], o[dt], 0, 0, 0);
+#pragma unroll
+        for (int i = PARTS - 1; i >= 0; --i)
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pb[i][uu], o[dt], 0, 0, 0);
       }
   };
   // (the queries and the first tiles are there: else the loop would wait for the queries, and with them for
@@ -334,14 +381,14 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
   }
   if (wave > 0) return;
   lsum += __shfl_xor(lsum, 32);
-  prefix_output<__bf16, D>(s, a, u, q, lane, m, lsum, o, reinterpret_cast<float*>(vbuf));
+  prefix_output<T, D>(s, a, u, q, lane, m, lsum, o, reinterpret_cast<float*>(vbuf));
 }
 
-template <int D>
+template <typename T, int D>
 __global__ __launch_bounds__(64 * kFewWaves, FewCfg<D>::WAVES) void k_attn_prefix4_few(DevState s, PrefixArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char vbuf[kFewWaves * FewCfg<D>::VBUF];
   __shared__ float ml[kFewWaves / 2 * 128];
-  few_wg<D>(s, a, vbuf, ml);
+  few_wg<T, D>(s, a, vbuf, ml);
 }
 
 // The same, and after prefix_wgs WGs those of the tries' own nodes, 64 rows each (32 of them rows).
@@ -354,7 +401,7 @@ __global__ __launch_bounds__(64 * kFewWaves, FewCfg<D>::WAVES) void k_attn_prefi
   __shared__ int wred[8];
   __shared__ float ml[256];
   if (blockIdx.x >= a.prefix_wgs) prefix_wg<D, 2, 2, Wgs::kTries, false>(s, a, buf[0], buf[1], kbuf1, vbuf1, wred, ml);
-  else few_wg<D>(s, a, buf[0], ml);
+  else few_wg<__bf16, D>(s, a, buf[0], ml);
 }
 
 template <int D>
@@ -370,7 +417,7 @@ void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, h
       return;
     }
   }
-  if (rpb == 32) hipExtLaunchKernelGGL(k_attn_prefix4_few<D>, grid, dim3(64 * kFewWaves), 0, st, ev0, ev1, 0, s, a);
+  if (rpb == 32) hipExtLaunchKernelGGL((k_attn_prefix4_few<__bf16, D>), grid, dim3(64 * kFewWaves), 0, st, ev0, ev1, 0, s, a);
   else if (rpb == 64) LAUNCH_PREFIX(2, 2, false);
   else LAUNCH_PREFIX(4, 1, false);
 #undef LAUNCH_PREFIX
@@ -379,6 +426,17 @@ void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, h
 }  // namespace
 
 hipError_t launch_prefix4(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
+  if (s.dtype == TD_F32) {
+    const dim3 grid(a.n_layers * s.Hkv * a.splits * a.row_blocks);
+    switch (s.D) {
+#define PREFIX_CASE(DD) \
+  case DD: hipExtLaunchKernelGGL((k_attn_prefix4_few<float, DD>), grid, dim3(64 * kFewWaves), 0, st, ev0, ev1, 0, s, a); break;
+      PREFIX_CASE(32) PREFIX_CASE(64) PREFIX_CASE(96) PREFIX_CASE(128)
+#undef PREFIX_CASE
+      default: return launch_prefix32(s, a, rows_per_block, st, ev0, ev1);
+    }
+    return hipGetLastError();
+  }
   switch (s.D) {
 #define PREFIX_CASE(DD) case DD: launch_d<DD>(s, a, rows_per_block, st, ev0, ev1); break;
     PREFIX_CASE(32) PREFIX_CASE(64) PREFIX_CASE(96) PREFIX_CASE(128)
