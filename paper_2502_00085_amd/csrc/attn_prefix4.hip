@@ -385,7 +385,7 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(64 * kFewWaves, FewCfg<D>::WAVES) void k_attn_prefix4_few(DevState s, PrefixArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, (sizeof(T) == 4 && D == 128 ? 1 : FewCfg<D>::WAVES)) void k_attn_prefix4_few(DevState s, PrefixArgs a) {
   __shared__ __attribute__((aligned(16))) unsigned char vbuf[kFewWaves * FewCfg<D>::VBUF];
   __shared__ float ml[kFewWaves / 2 * 128];
   few_wg<T, D>(s, a, vbuf, ml);
@@ -432,6 +432,7 @@ hipError_t launch_prefix4(const DevState& s, const PrefixArgs& a, int rows_per_b
 #define PREFIX_CASE(DD) \
   case DD: hipExtLaunchKernelGGL((k_attn_prefix4_few<float, DD>), grid, dim3(64 * kFewWaves), 0, st, ev0, ev1, 0, s, a); break;
       PREFIX_CASE(32) PREFIX_CASE(64) PREFIX_CASE(96) PREFIX_CASE(128)
+      PREFIX_CASE(160) PREFIX_CASE(192) PREFIX_CASE(224) PREFIX_CASE(256)
 #undef PREFIX_CASE
       default: return launch_prefix32(s, a, rows_per_block, st, ev0, ev1);
     }
