@@ -159,13 +159,17 @@ __global__ __launch_bounds__(kMergeThreads) void k_prefix_merge(DevState s, Pref
 
 }  // namespace
 
-// A 4-bit pass in bf16 of up to 512 rows takes them 32 at a time (k_attn_prefix4_few): measured against blocks of
-// up to 128, us, with the splits below, 8 KV heads at d = 128 unless stated: 64 rows over 4,096 keys 17.1 and
-// 18.7, over 30,000 29.6 and 35; 128 rows 19.7 and 22.5, 40.3 and 42.6; 512 rows 30.7 and 33.1, over 20,000 77.9 and
-// 75.3; 1,024 rows 43.4 and 43.2, 125 and 119; 32 KV heads, 128 rows over 20,000 73.4 and 87; at d = 256 256 rows
-// over 20,000 99 and 69.
+// A 4-bit pass takes its rows 32 at a time (k_attn_prefix4_few) in bf16 up to 512 of them and d = 128.  Measured
+// against blocks of up to 128, us, with the splits below, 8 KV heads at d = 128 unless stated: 64 rows over 4,096
+// keys 17.1 and 18.7, over 30,000 29.6 and 35; 128 rows 19.7 and 22.5, 40.3 and 42.6; 512 rows 30.7 and 33.1, over
+// 20,000 77.9 and 75.3; 1,024 rows 43.4 and 43.2, 125 and 119; 32 KV heads, 128 rows over 20,000 73.4 and 87; at d = 256
+// 256 rows over 20,000 99 and 69.  In fp32 any number up to d = 192, against the fp32 matrix instructions
+// (k_attn_prefix32): d = 128, 128 rows over 8,000 45.6 and 104; d = 192, 4 KV heads, 57 and 84; d = 256, 116 and 102.
+static bool few_rows(const DevState& s, bool four, long rows) {
+  return four && (s.dtype == TD_F32 ? s.D <= 192 : s.D <= 128 && rows <= 512);
+}
 int prefix_rows_per_block(const DevState& s, bool four, long rows) {
-  if (four && s.D <= 128 && (rows <= 512 || s.dtype == TD_F32)) return 32;
+  if (few_rows(s, four, rows)) return 32;
   return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
 }
 
@@ -183,9 +187,10 @@ int prefix_rows_per_block(const DevState& s, bool four, long rows) {
 // KV heads, 8 rows over 30,000, 4 / 8 / 16: 60.5 / 39.3 / 42.8; 128 rows over 20,000 (313 tiles), 2 / 4: 85 / 73.4.
 int prefix_splits(const DevState& s, bool four, long units, long keys, long most) {
   const long tiles = (keys + 63) / 64;
-  if (four && s.D <= 128) {
+  if (few_rows(s, four, 0)) {
     const long least = units < 16 ? 4 : 6;
-    const long one = std::min(256 / units, (tiles + least - 1) / least), two = std::min(512 / units, tiles / 64);
+    const long one = std::min(256 / units, (tiles + least - 1) / least);
+    const long two = s.dtype == TD_F32 && s.D >= 128 ? 0 : std::min(512 / units, tiles / 64);  // (fp32: one fits a CU)
     return (int)std::max(1l, std::min(std::max(one, two), most));
   }
   const long few = s.dtype == TD_F32 ? 1 : 4, many = s.dtype == TD_F32 ? 2 : 16;

@@ -432,7 +432,7 @@ hipError_t launch_prefix4(const DevState& s, const PrefixArgs& a, int rows_per_b
 #define PREFIX_CASE(DD) \
   case DD: hipExtLaunchKernelGGL((k_attn_prefix4_few<float, DD>), grid, dim3(64 * kFewWaves), 0, st, ev0, ev1, 0, s, a); break;
       PREFIX_CASE(32) PREFIX_CASE(64) PREFIX_CASE(96) PREFIX_CASE(128)
-      PREFIX_CASE(160) PREFIX_CASE(192) PREFIX_CASE(224) PREFIX_CASE(256)
+      PREFIX_CASE(160) PREFIX_CASE(192)
 #undef PREFIX_CASE
       default: return launch_prefix32(s, a, rows_per_block, st, ev0, ev1);
     }
