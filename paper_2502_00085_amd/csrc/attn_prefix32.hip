@@ -372,11 +372,18 @@ hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_
   switch (s.D) {
 #define PREFIX_CASE(DD)                                                       \
   case DD:                                                                    \
+    if (!a.four) launch_d<DD, false>(s, a, rows_per_block, st, ev0, ev1);     \
+    else return hipErrorInvalidValue;                                         \
+    break;
+    PREFIX_CASE(32) PREFIX_CASE(64) PREFIX_CASE(96) PREFIX_CASE(128)
+    PREFIX_CASE(160) PREFIX_CASE(192)
+#undef PREFIX_CASE
+#define PREFIX_CASE(DD)                                                       \
+  case DD:                                                                    \
     if (a.four) launch_d<DD, true>(s, a, rows_per_block, st, ev0, ev1);       \
     else launch_d<DD, false>(s, a, rows_per_block, st, ev0, ev1);             \
     break;
-    PREFIX_CASE(32) PREFIX_CASE(64) PREFIX_CASE(96) PREFIX_CASE(128)
-    PREFIX_CASE(160) PREFIX_CASE(192) PREFIX_CASE(224) PREFIX_CASE(256)
+    PREFIX_CASE(224) PREFIX_CASE(256)
 #undef PREFIX_CASE
     default: return hipErrorInvalidValue;
   }

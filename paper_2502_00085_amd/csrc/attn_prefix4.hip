@@ -412,14 +412,21 @@ void launch_d(const DevState& s, const PrefixArgs& a, int rpb, hipStream_t st, h
   if constexpr (D == 64 || D == 96 || D == 128) {
     if (a.trie_splits > 0) {
       if (rpb == 32) hipExtLaunchKernelGGL(k_attn_prefix4_few_tries<D>, grid, dim3(64 * kFewWaves), 0, st, ev0, ev1, 0, s, a);
-      else if (rpb == 64) LAUNCH_PREFIX(2, 2, true);
       else LAUNCH_PREFIX(4, 1, true);
       return;
     }
   }
-  if (rpb == 32) hipExtLaunchKernelGGL((k_attn_prefix4_few<__bf16, D>), grid, dim3(64 * kFewWaves), 0, st, ev0, ev1, 0, s, a);
-  else if (rpb == 64) LAUNCH_PREFIX(2, 2, false);
-  else LAUNCH_PREFIX(4, 1, false);
+  if (rpb == 32) {
+    hipExtLaunchKernelGGL((k_attn_prefix4_few<__bf16, D>), grid, dim3(64 * kFewWaves), 0, st, ev0, ev1, 0, s, a);
+    return;
+  }
+  if constexpr (D > 128) {  // (up to d = 128 more than 32 rows to a block are more than 512)
+    if (rpb == 64) {
+      LAUNCH_PREFIX(2, 2, false);
+      return;
+    }
+  }
+  LAUNCH_PREFIX(4, 1, false);
 #undef LAUNCH_PREFIX
 }
 

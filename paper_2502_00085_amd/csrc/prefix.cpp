@@ -21,6 +21,7 @@ constexpr int kFoldSplits = 4;
 constexpr long kOneRound = 512;  // WGs of a pass that run at once (two per CU)
 constexpr long kTrieTiles = 8;
 constexpr long kShortPass = 16;  // tiles of the prefix per WG
+constexpr long kSmallBlocks = 1 << 20;  // blocks of 32 rows (of a layer) per launch
 constexpr int kStoreRows = 1 << 26;  // rows per layer of a store (what a launch's grid holds)
 constexpr size_t kWorkFloats = 16u << 20;  // of either workspace, unless one layer needs more
 
@@ -385,47 +386,53 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
   const int rpb = td::prefix_rows_per_block(s, c->prefix_four, rows), blocks = (int)((rows + rpb - 1) / rpb);
   // (as many layers per launch as its grid holds)
   const int lc = (int)std::max(1l, std::min<long>(n_layers, (1l << 22) / ((long)s.Hkv * blocks)));
+  // (and as many queries: blocks of 32 rows, which a 4-bit pass in fp32 takes any number of, may come to more)
+  const int qc = rpb > 32 || (long)s.Hkv * blocks <= kSmallBlocks ? n : (int)std::max(1l, kSmallBlocks / s.Hkv * rpb / G);
   const size_t layer = (size_t)n * s.Hq * s.D * (s.dtype == TD_F32 ? 4 : 2);
   hipEvent_t ev0 = c->ev[TD_PHASE_ATTN][0], ev1 = c->ev[TD_PHASE_ATTN][1];
   c->ev[TD_PHASE_ATTN][0] = c->ev[TD_PHASE_ATTN][1] = nullptr;
   hipError_t e = hipSuccess;
   for (int l = 0; l < n_layers && e == hipSuccess; l += lc) {
-    td::PrefixArgs a{};
-    a.q = static_cast<const char*>(d_q) + l * layer;
-    a.out = static_cast<char*>(d_out) + l * layer;
-    a.rows = td::PrefixRows::kChunk;
-    a.four = c->prefix_four;
-    a.layer_begin = layer_begin + l;
-    a.n_layers = std::min(lc, n_layers - l);
-    a.tries = 1;
-    a.per_trie = a.q_stride = n;
-    a.pos0 = pos;
-    a.scale_log2 = scale * 1.4426950408889634f;
-    a.row_blocks = blocks;
-    const long keys = s.W > 0 ? std::min(pos + n, s.W) : pos + n, units = (long)a.n_layers * s.Hkv * blocks;
-    const long fit = (long)(c->prefix_records / ((size_t)a.n_layers * n * s.Hq));
-    a.records = a.splits = td::prefix_splits(s, a.four && rpb == 32, units, keys, std::max(1l, fit));
-    a.xcd_group = blocks > 1 && ((long)a.n_layers * s.Hkv * a.splits) % 8 == 0;
-    // Two WGs per CU at once, and no third: a long block beside a short one.  2,048 tokens of 32 heads (8
-    // KV heads, d = 128) from position 0: 57.5 -> 53.7 us a layer, from 6,144: 254 -> 247.5 (graphs in turn);
-    // where fewer CUs have two (1,500 tokens) 42.4 -> 41.4 from 0, 210.4 and 210.7 from 6,144.  With more WGs the
-    // longest first fill the CUs evenly by themselves.
-    a.pair_blocks = s.D <= 128 && units * a.splits > kOneRound / 2 && units * a.splits <= kOneRound;
-    a.part_o = a.splits > 1 ? c->prefix_o : nullptr;
-    a.part_ml = c->prefix_ml;
-    hipEvent_t last = l + lc >= n_layers ? ev1 : nullptr;
-    e = td::launch_prefix(s, a, st, l == 0 ? ev0 : nullptr, a.part_o ? nullptr : last);
-    if (e == hipSuccess && a.part_o) {
-      td::PrefixMergeArgs m{};
-      m.prefix_o = c->prefix_o;
-      m.prefix_ml = c->prefix_ml;
-      m.prefix_splits = a.splits;
-      m.out = a.out;
-      m.rows = td::PrefixRows::kChunk;
-      m.n_layers = a.n_layers;
-      m.tries = 1;
-      m.per_trie = n;
-      e = td::launch_prefix_merge(s, m, st, last);
+    for (int q0 = 0; q0 < n && e == hipSuccess; q0 += qc) {
+      td::PrefixArgs a{};
+      a.q = static_cast<const char*>(d_q) + l * layer;
+      a.out = static_cast<char*>(d_out) + l * layer;
+      a.rows = td::PrefixRows::kChunk;
+      a.four = c->prefix_four;
+      a.layer_begin = layer_begin + l;
+      a.n_layers = std::min(lc, n_layers - l);
+      a.tries = 1;
+      a.q0 = q0;
+      a.per_trie = std::min(qc, n - q0);
+      a.q_stride = n;
+      a.pos0 = pos;
+      a.scale_log2 = scale * 1.4426950408889634f;
+      a.row_blocks = qc == n ? blocks : (int)(((long)a.per_trie * G + rpb - 1) / rpb);
+      const long keys = s.W > 0 ? std::min(pos + n, s.W) : pos + n, units = (long)a.n_layers * s.Hkv * a.row_blocks;
+      const long fit = qc == n ? (long)(c->prefix_records / ((size_t)a.n_layers * n * s.Hq)) : 1;
+      a.records = a.splits = td::prefix_splits(s, a.four && rpb == 32, units, keys, std::max(1l, fit));
+      a.xcd_group = a.row_blocks > 1 && ((long)a.n_layers * s.Hkv * a.splits) % 8 == 0;
+      // Two WGs per CU at once, and no third: a long block beside a short one.  2,048 tokens of 32 heads (8
+      // KV heads, d = 128) from position 0: 57.5 -> 53.7 us a layer, from 6,144: 254 -> 247.5 (graphs in turn);
+      // where fewer CUs have two (1,500 tokens) 42.4 -> 41.4 from 0, 210.4 and 210.7 from 6,144.  With more WGs the
+      // longest first fill the CUs evenly by themselves.
+      a.pair_blocks = s.D <= 128 && units * a.splits > kOneRound / 2 && units * a.splits <= kOneRound;
+      a.part_o = a.splits > 1 ? c->prefix_o : nullptr;
+      a.part_ml = c->prefix_ml;
+      hipEvent_t last = l + lc >= n_layers && q0 + qc >= n ? ev1 : nullptr;
+      e = td::launch_prefix(s, a, st, l == 0 && q0 == 0 ? ev0 : nullptr, a.part_o ? nullptr : last);
+      if (e == hipSuccess && a.part_o) {  // (of all queries)
+        td::PrefixMergeArgs m{};
+        m.prefix_o = c->prefix_o;
+        m.prefix_ml = c->prefix_ml;
+        m.prefix_splits = a.splits;
+        m.out = a.out;
+        m.rows = td::PrefixRows::kChunk;
+        m.n_layers = a.n_layers;
+        m.tries = 1;
+        m.per_trie = n;
+        e = td::launch_prefix_merge(s, m, st, last);
+      }
     }
   }
   if (e != hipSuccess) return hip_fail(c, e, "trie_prefix_attn launch");

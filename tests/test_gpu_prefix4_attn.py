@@ -94,9 +94,57 @@ def test_layers_past_the_workspace():
 @pytest.mark.parametrize("D,Hq,Hkv,b,tries,S,L", [(128, 8, 2, 4, [(300, 6), (20, 2)], 1500, 1), (128, 8, 2, 6, [(200, 6), (20, 2)], 1500, 1),
                                                   (128, 8, 2, 16, [(100, 3), (20, 2), (64, 1)], 1500, 1), (64, 16, 4, 16, [(200, 8)] * 12, 130, 4),
                                                   (96, 8, 8, 3, [(1500, 4), (90, 2)], 40, 1), (96, 8, 8, 30, [(150, 4), (90, 2)], 400, 1),
+                                                  (128, 8, 1, 40, [(30, 2), (64, 1)], 300, 1), (64, 24, 2, 30, [(50, 1)] * 2, 900, 1),
                                                   (64, 4, 4, 20, [(150, 4), (90, 2)], 400, 1), (128, 32, 8, 40, [(30, 3), (64, 1)], 700, 2)])
 def test_where_the_nodes_go(D, Hq, Hkv, b, tries, S, L):
     Batch("bf16", D, Hq, Hkv, S, 64, tries, b, L=L, dead=True).decode(sample=0.05 if len(tries) > 3 else 0.3)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 96), ("bf16", 128), ("bf16", 160), ("bf16", 256), ("f32", 96), ("f32", 192), ("f32", 224)])
+@pytest.mark.parametrize("off", [1, 3])
+def test_scales_at_any_address(dtype, D, off):
+    """Scale bytes that begin at an odd address."""
+    bt = Batch(dtype, D, 4, 2, 200, 16, [(9, 2), (20, 1)], 3)
+    p = bt.prefix
+    keep = []
+    for name in ("k", "v"):
+        e, s = getattr(p, name)
+        moved = torch.zeros(s.numel() + 8, dtype=torch.uint8, device="cuda")[off:off + s.numel()].view(s.shape)
+        moved.copy_(s)
+        keep.append(s)
+        setattr(p, name, (e, moved))
+    p.attach(bt.dec)
+    for s in keep:
+        s.fill_(255)  # (no longer read)
+    bt.decode()
+
+
+def test_fp32_chunk_in_several_launches():
+    """More blocks of rows than a launch takes: two launches over the queries.  Rows at either side of the border,
+    of the ends, and some between."""
+    D, Hkv, G, n, W, page = 32, 8, 8, 530_000, 50, 4096
+    dec = B.TrieDecoder(1, 1, 4, 100, 1, Hkv * G, Hkv, D, W, "f32")
+    gen, rng = torch.Generator().manual_seed(5), np.random.default_rng(5)
+    n_pages = -(-n // page)
+    e = [torch.randint(0, 256, (n_pages, 1, Hkv, page, D // 2), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    s = [torch.randint(124, 128, (n_pages, 1, Hkv, page, 1), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    dec.set_prefix4(e[0], s[0], e[1], s[1], range(n_pages), n)
+    q = torch.empty((1, n, Hkv * G, D), device="cuda").normal_()
+    out = torch.full_like(q, 9.0)
+    dec.prefix_attn(0, 1, 0, q, out, 0.2)
+    assert dec.status() == 0
+    border = (1 << 20) // Hkv * 32 // G
+    assert 0 < border < n
+    at = [0, 1, 49, 50, border - 1, border, border + 1, n - 1] + [int(x) for x in rng.integers(0, n, 12)]
+    for j in at:
+        lo = max(0, j - W + 1)
+        k, v = (values64(x[lo // page:j // page + 1, 0].transpose(1, 2).flatten(0, 1)[lo % page:lo % page + j - lo + 1],
+                         y[lo // page:j // page + 1, 0].transpose(1, 2).flatten(0, 1)[lo % page:lo % page + j - lo + 1]).transpose(0, 1)
+                for x, y in zip(e, s))
+        want, tol = plain.attend(q[0, j:j + 1], k, v, torch.ones(1, j - lo + 1, dtype=torch.bool), 0.2, torch.float32)
+        check(out[0, j:j + 1], want, tol, j)
+    assert not bool((out == 9.0).all(-1).any())
+    dec.close()
 
 
 def test_leaves_stored_by_the_call():
