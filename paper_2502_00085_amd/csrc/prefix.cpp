@@ -119,8 +119,6 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * s.T * qn * s.Hq));
   a.four = c->prefix_four;
   a.splits = prefix_splits(s, a.four && rpb == 32, (long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
-  a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
-  a.records = a.splits;
   *tries = false;
   if (trie_nodes > 0) {
     // the tries' own nodes in the same launch, where all of its WGs run at once, none has more than
@@ -134,17 +132,24 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
     // over 30,000 positions 38.9 us in one launch of 8 or 12 splits, 42.7 in two of 16.
     // A trie's WG has 3 of its tiles, which take about as long as the 4 that a WG of the prefix has at least:
     // over 160 of these shapes 1 or 2 took 1.4 % less in the mean, 4 took 4 % more, 6 8 %, 8 13 %.
-    const long wgs = (long)n_layers * s.Hkv * a.row_blocks * a.splits, tiles = (trie_nodes + 63) / 64;
+    const long unit = (long)n_layers * s.Hkv * a.row_blocks, tiles = (trie_nodes + 63) / 64, prefix_tiles = (keys + 63) / 64;
     const long blocks = (qn * (s.Hq / s.Hkv) + rpb - 1) / rpb, units = (long)n_layers * s.T * s.Hkv * blocks;
     const long ts = std::max(1l, std::min({(tiles + 2) / 3, 256 / units, fit - a.splits}));
-    if (wgs + units * ts <= kOneRound && (a.four || (keys + 63) / 64 <= (long)kShortPass * a.splits) && (tiles + ts - 1) / ts <= kTrieTiles && a.splits + ts <= fit) {
+    // In 4 bits and blocks of 32 rows a short pass leaves CUs to the tries (128 rows over 4,096 keys, 6 splits 19.9 us, 8
+    // 21.5; 64 rows over 8,000, 14 22.8, 16 25.1; 8 rows of 32 KV heads, d = 96, over 8,000, 21 tiles per WG, 6 23.8, 8
+    // 22.5).
+    const long left = std::max(0l, 256 - units * ts) / unit;
+    if (a.four && rpb == 32 && prefix_tiles <= kShortPass * left) a.splits = (int)std::min<long>(a.splits, left);
+    const long wgs = unit * a.splits;
+    if (wgs + units * ts <= kOneRound && (a.four || prefix_tiles <= kShortPass * a.splits) && (tiles + ts - 1) / ts <= kTrieTiles && a.splits + ts <= fit) {
       a.trie_splits = (int)ts;
       a.trie_blocks = (int)blocks;
       a.prefix_wgs = (uint32_t)wgs;
-      a.records = a.splits + a.trie_splits;
       *tries = true;
     }
   }
+  a.records = a.splits + a.trie_splits;
+  a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
   *splits = a.records;
   return launch_prefix(s, a, st, ev0, nullptr);
 }
