@@ -1,9 +1,23 @@
-// Attention over a shared prefix in 4 bits (gfx950 matrix cores, bf16 queries, fp32 accumulate).
+// Attention over a shared prefix in 4 bits (gfx950 matrix cores, fp32 accumulate).
 //
-// The contract, the products and the softmax are those of k_attn_prefix (attn_prefix.hip); a key's values are
-// its 4-bit sizes times the block's unit, exact in bf16, so that nothing is rounded on the way to the matrix
-// cores.  A conversion makes two of them from a byte (v_cvt_scalef32_pk_bf16_fp4): 32 per lane for 32 keys of K or
-// V at d = 128.
+// The contract, the products and the softmax are those of k_attn_prefix (attn_prefix.hip); a key's values are its
+// 4-bit sizes times the block's unit, exact in bf16, so that nothing is rounded on the way to the matrix cores.  A
+// conversion makes two of them from a byte (v_cvt_scalef32_pk_bf16_fp4): 32 per lane for 32 keys of K or V at d = 128.
+//
+//   * More than 512 rows per KV head (a prefill): k_attn_prefix4, in blocks of up to 128 rows.  A tile is converted once
+//     for all of them, on its way into LDS, and multiplied as a bf16 one.  Bound by the clock under matrix load, as
+//     in bf16: 2,048 tokens from position 6,144 (8 KV heads, 32 query heads, d = 128) 237 us a layer, 1,012 TFLOP/s
+//     (without a trace 232, 1,036; the bf16 prefix 241, a library product 1,252).
+//   * Fewer (a decode step): k_attn_prefix4_few, in blocks of 32 rows.  HBM where the prefix is long: 8 rows of 32
+//     KV heads, d = 96, over 50,001 positions 36.4 us, 4.5 TB/s (a copy's 4.9), 43 with the tries' nodes in the launch
+//     (the bf16 pass 108 to 112).  Below some 4,000 keys per KV head a chain of latencies, as in bf16: 128 rows of 8 KV
+//     heads over 4,096 keys, with the tries' nodes, 16.9 us (its 4.5 MB take 0.9, its records 2 to 3).
+//   * fp32: the same kernel, the queries and the weights as three bf16 parts each (24 bits: all of them), three products
+//     for one.  These run at 5 times the rate of the fp32 matrix instructions or more: 700 tokens from position
+//     3,000 (32 heads, d = 128) 134 us against 520; 128 rows of 8 KV heads over 8,000 keys 23.6 against 80.
+// Tried and not kept: eight waves per WG (the same to 1 %; more than 256 registers a wave past d = 128); one tile's loads
+// under way instead of two, which the compiler made of them while the queries' loads were not waited for ahead of the
+// loop (48.9 us for the 36.4 above).
 #include <algorithm>
 #include <type_traits>
 
@@ -391,10 +405,11 @@ __global__ __launch_bounds__(64 * kFewWaves, (sizeof(T) == 4 && D == 128 ? 1 : F
   few_wg<T, D>(s, a, vbuf, ml);
 }
 
-// The same, and after prefix_wgs WGs those of the tries' own nodes, 64 rows each (32 of them rows).
+// The same, and after prefix_wgs WGs those of the tries' own nodes, kFewTrieRows rows of a trie each.
 template <int D>
 __global__ __launch_bounds__(64 * kFewWaves, FewCfg<D>::WAVES) void k_attn_prefix4_few_tries(DevState s, PrefixArgs a) {
   using C = PrefixCfg<D, 2, 2>;
+  static_assert(kFewTrieRows == 64, "two waves of 32 rows");
   static_assert(C::THREADS == 64 * kFewWaves && 2 * C::BUF == kFewWaves * FewCfg<D>::VBUF, "the same WG");
   __shared__ __attribute__((aligned(16))) unsigned char buf[2][C::BUF];
   __shared__ __attribute__((aligned(16))) unsigned char kbuf1[C::BUF], vbuf1[C::BUF];

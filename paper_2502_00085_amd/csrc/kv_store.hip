@@ -14,7 +14,8 @@
 // What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape (201 MB in and out) in 43.4 us (the
 // least 38.1), 4.6 TB/s (5.3; a copy's 5.0); with few rows one launch's latency (the leaves of 16 tries of 16
 // beams, 6.3 MB, 4.3 us; the least 4.1).  Rows are read and written once; up to 8 of one layer share a WG, so that the
-// angles are computed once for the 32 to 48 heads of a row.
+// angles are computed once for the 32 to 48 heads of a row.  With several axes the same: 6,001 tokens of a layer, 147 MB,
+// 28.8 us, 5.1 TB/s.
 #include <algorithm>
 
 #include "kv_rows.h"

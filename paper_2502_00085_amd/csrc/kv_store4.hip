@@ -10,6 +10,10 @@
 // of the eight sizes an error of 2^-24 would move the element by up to half its size.  On its way a value
 // passes through fp32, rounded to odd in 20 bits (the low bit stands for all that was cut off): no border
 // and no tie lies between it and the exact one.
+//
+// What bounds it: HBM, once the sines are there.  8,192 tokens of a layer at the Llama-8B shape, queries too (100 MB in,
+// 76 out), 40.2 to 42.2 us, 4.2 to 4.4 TB/s (a copy's 4.9): its 1,024 WGs all compute the 64-bit sines and cosines of their
+// 8 rows first, once for the 48 heads of a row.
 #include <algorithm>
 
 #include "kv_rows.h"

@@ -119,6 +119,17 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * s.T * qn * s.Hq));
   a.four = c->prefix_four;
   a.splits = prefix_splits(s, a.four && rpb == 32, (long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
+  // In 4 bits, row blocks that read the same keys belong on one XCD, if that costs less than a fifth of the splits (us, over
+  // 30,000 positions: 16 beams, 4 KV heads, d = 64, 30 splits 20.1, 31 21.5; 8 x 16 beams, 28 heads and 4 KV heads, d = 128,
+  // 97.5 and 124.6; 8 x 16 beams of 6 heads, d = 96, 8 splits 38.7, 10 36.3).
+  auto group = [&]() {
+    for (int i = a.splits; a.four && a.row_blocks > 1 && 5 * i > 4 * a.splits; --i)
+      if ((long)n_layers * s.Hkv * i % 8 == 0) {
+        a.splits = i;
+        break;
+      }
+  };
+  group();
   *tries = false;
   if (trie_nodes > 0) {
     // the tries' own nodes in the same launch, where all of its WGs run at once, none has more than
@@ -133,13 +144,17 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
     // A trie's WG has 3 of its tiles, which take about as long as the 4 that a WG of the prefix has at least:
     // over 160 of these shapes 1 or 2 took 1.4 % less in the mean, 4 took 4 % more, 6 8 %, 8 13 %.
     const long unit = (long)n_layers * s.Hkv * a.row_blocks, tiles = (trie_nodes + 63) / 64, prefix_tiles = (keys + 63) / 64;
-    const long blocks = (qn * (s.Hq / s.Hkv) + rpb - 1) / rpb, units = (long)n_layers * s.T * s.Hkv * blocks;
+    const int tr = a.four && rpb == 32 ? kFewTrieRows : rpb;  // a trie's rows of a WG
+    const long blocks = (qn * (s.Hq / s.Hkv) + tr - 1) / tr, units = (long)n_layers * s.T * s.Hkv * blocks;
     const long ts = std::max(1l, std::min({(tiles + 2) / 3, 256 / units, fit - a.splits}));
     // In 4 bits and blocks of 32 rows a short pass leaves CUs to the tries (128 rows over 4,096 keys, 6 splits 19.9 us, 8
     // 21.5; 64 rows over 8,000, 14 22.8, 16 25.1; 8 rows of 32 KV heads, d = 96, over 8,000, 21 tiles per WG, 6 23.8, 8
     // 22.5).
     const long left = std::max(0l, 256 - units * ts) / unit;
-    if (a.four && rpb == 32 && prefix_tiles <= kShortPass * left) a.splits = (int)std::min<long>(a.splits, left);
+    if (a.four && rpb == 32 && prefix_tiles <= kShortPass * left && left < a.splits) {
+      a.splits = (int)left;
+      group();
+    }
     const long wgs = unit * a.splits;
     if (wgs + units * ts <= kOneRound && (a.four || prefix_tiles <= kShortPass * a.splits) && (tiles + ts - 1) / ts <= kTrieTiles && a.splits + ts <= fit) {
       a.trie_splits = (int)ts;

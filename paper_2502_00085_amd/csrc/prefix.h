@@ -51,6 +51,7 @@ hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st,
 hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
                            hipEvent_t ev1);
 
+constexpr int kFewTrieRows = 64;  // rows of a trie's WG beside a 4-bit pass in blocks of 32 rows
 hipError_t launch_prefix4(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
                           hipEvent_t ev1);
 
