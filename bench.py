@@ -41,8 +41,8 @@ HBM_PEAK_GBS = 8000.0
 ATTN_TRAFFIC = {
     "workload": "llama8b",
     "profile": "profiles/k_attn_mfma_llama8b_hbm_traffic.md",
-    "sources_sha256": "a90fb0954cf7fb7d81a8facba62e617bc5d5d14f43f8255df866b2e5162e58f6",
-    "bytes_per_launch": 275910400,    # 2.0 x 133,697.88 KiB FETCH_SIZE + 1.0 x 2,048 KiB WRITE_SIZE
+    "sources_sha256": "258ccbae959d11bc78589f9768f969e5e17ebafd3305585c53aebedf8054bc82",
+    "bytes_per_launch": 275910144,    # 2.0 x 133,697.75 KiB FETCH_SIZE + 1.0 x 2,048 KiB WRITE_SIZE
     "nodes_per_launch": 2070,         # attended nodes of the profiled (step-10) trie
     "qo_bytes_per_launch": 4194304,   # queries + outputs of the profiled launch
 }
