@@ -235,7 +235,8 @@ typedef struct {
  * prefix is attached at a time, of either kind; trie_prefix_store, trie_prefix_load, trie_prefix_attn and the
  * tries' attention then work on 4-bit positions: trie_prefix_store rounds K (rotated, in 64 bits) and V to 4
  * bits once; the attention multiplies the values that the stored rows stand for, which bf16 holds exactly
- * (past fp32's range: infinite), in the context's type as ever.  The tries' own nodes stay in the context's type.
+ * (past fp32's range, units of 2^126 and 2^127, which no store writes: infinite, in fp32 outputs infinite or NaN),
+ * in the context's type as ever.  The tries' own nodes stay in the context's type.
  *   Rounding.  m = 2^k f (1 <= f < 2), the largest size of a block, has the unit 2^(k - 2), or 2^(k - 1) where f
  *   >= 1.75, within 2^-125 and 2^125 (a block of zeros 2^-125); an element is the nearest of the eight sizes of
  *   units, ties to the even code, past 6 as 6.  A block with an infinity (also: past fp32's range after the
