@@ -285,7 +285,7 @@ td_status trie_prefix_store_axes(td_ctx* ctx, int32_t layer_begin, int32_t n_lay
 
 /* Rows of the prefix back, as the values that are stored (K rotated): positions pos .. pos + n - 1, n <= 2^26
  * (inside the table; `length` plays no part), into d_k and d_v [nl][n][Hkv][d], desc.dtype; either may be NULL.
- * From 4-bit pages the values are exact.  Needs an attached prefix (else TD_ESTATE), but no prompts. */
+ * From 4-bit pages the values are exact (those below 2^-126 may be 0).  Needs an attached prefix (else TD_ESTATE), but no prompts. */
 td_status trie_prefix_load(td_ctx* ctx, int32_t layer_begin, int32_t n_layers, int32_t pos, int32_t n, void* d_k,
                            void* d_v, hipStream_t stream);
 

@@ -9,6 +9,7 @@ namespace td {
 
 constexpr int kStoreThreads = 256;
 constexpr int kStoreRows = 8;    // rows of a WG at most
+constexpr long kStoreMany = 1 << 22;  // rows of a layer from which on a WG has that many
 constexpr int kStorePairs = 128;  // of a head
 
 template <typename T>

@@ -11,11 +11,12 @@
 // The angle of a far position needs more than fp32: p f_i in turns, in 64 bits, less whole turns;
 // the sine and cosine of the rest in fp32, once per (row, pair), in LDS for all of the row's heads.
 //
-// What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape (201 MB in and out) in 43.4 us (the
-// least 38.1), 4.6 TB/s (5.3; a copy's 5.0); with few rows one launch's latency (the leaves of 16 tries of 16
-// beams, 6.3 MB, 4.3 us; the least 4.1).  Rows are read and written once; up to 8 of one layer share a WG, so that the
-// angles are computed once for the 32 to 48 heads of a row.  With several axes the same: 6,001 tokens of a layer, 147 MB,
-// 28.8 us, 5.1 TB/s.
+// What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape (201 MB in and out) in 40.7 us, 4.9 TB/s
+// (a copy's 4.9); with few rows one launch's latency (the leaves of 16 tries of 16 beams, 6.3 MB, 4.3 us; the
+// least 4.1).  Rows are read and written once; a WG has one, so that the angles are computed once
+// for its 32 to 48 heads.  With several rows to a WG the CUs end one after another (2 layers, eager, 1 / 2 / 4 / 8 rows, us:
+// 8,192 tokens 81.8 / 85.1 / 85.9 / 88.3; 16,000 149 / 156 / 160 / 172; 8 ragged prompts 64.3 / 64.1 / 71.5 / 76.7).  With several
+// axes the same: 6,001 tokens of a layer, 147 MB, 30.3 us, 4.9 TB/s.
 #include <algorithm>
 
 #include "kv_rows.h"
@@ -24,7 +25,7 @@ namespace td {
 
 namespace {
 
-// Grid (row groups, layers); a WG takes `group` consecutive rows (trie, j) of one layer.
+// Grid (row groups, layers); a WG takes `group` consecutive rows (trie, j) of one layer: one, or of very many rows several.
 template <typename T, bool AXES>
 __global__ __launch_bounds__(kStoreThreads) void k_store(DevState s, StoreArgs a, int group) {
   using C = StoreCfg<T>;
@@ -92,14 +93,15 @@ __global__ __launch_bounds__(kStoreThreads) void k_store(DevState s, StoreArgs a
 
 }  // namespace
 
-int store_group(long rows, int n_layers) {
-  // (as many rows per WG as leave a few WGs per CU)
-  return (int)std::max(1l, std::min<long>(kStoreRows, rows * n_layers / 1024));
+int store_group(long rows, int n_layers, int most) {
+  // (as many rows per WG as leave a few WGs per CU, at most `most`; a grid of hundreds of millions of threads is long enough)
+  if (rows > kStoreMany) return kStoreRows;
+  return (int)std::max(1l, std::min<long>(most, rows * n_layers / 1024));
 }
 
 hipError_t launch_store(const DevState& s, const StoreArgs& a, hipStream_t st) {
   const long rows = (long)a.tries * a.n;
-  const int group = store_group(rows, a.n_layers);
+  const int group = store_group(rows, a.n_layers, 1);
   const dim3 grid((rows + group - 1) / group, a.n_layers);
 #define LAUNCH_STORE(T, AXES) hipLaunchKernelGGL((k_store<T, AXES>), grid, dim3(kStoreThreads), 0, st, s, a, group)
   const bool f32 = s.dtype == TD_F32;

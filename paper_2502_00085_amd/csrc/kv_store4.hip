@@ -11,9 +11,9 @@
 // passes through fp32, rounded to odd in 20 bits (the low bit stands for all that was cut off): no border
 // and no tie lies between it and the exact one.
 //
-// What bounds it: HBM, once the sines are there.  8,192 tokens of a layer at the Llama-8B shape, queries too (100 MB in,
-// 76 out), 40.2 to 42.2 us, 4.2 to 4.4 TB/s (a copy's 4.9): its 1,024 WGs all compute the 64-bit sines and cosines of their
-// 8 rows first, once for the 48 heads of a row.
+// What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape, queries too (100 MB in, 76 out), 37.3 to 41 us, 4.3
+// to 4.7 TB/s (a copy's 4.9), with two rows to a WG; eight of them 40.8 to 44.5, one took 7 % longer (2 layers).  The 64-bit
+// sines are computed once for the 48 heads of a row; V's loads under way meanwhile changed nothing.
 #include <algorithm>
 
 #include "kv_rows.h"
@@ -23,7 +23,6 @@ namespace td {
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
 
 __device__ inline float to_odd(double x) {
   const uint64_t u = __builtin_bit_cast(uint64_t, x);
@@ -141,8 +140,8 @@ __global__ __launch_bounds__(kStoreThreads) void k_store4(DevState s, StoreArgs 
 }
 
 // Grid (row groups, layers); units of 8 elements of a row, K's and then V's, four under way per thread.  Bound by
-// HBM: 8,192 tokens of 8 heads at d = 128, 42 MB in and out, 11.1 us (3.8 TB/s); K and V in one loop, of batches of 4 or
-// 8, 12.1.
+// HBM: 8,192 tokens of 8 heads at d = 128, 42 MB in and out, 11.1 us (3.8 TB/s) with 8 rows to a
+// WG, two 17.5; K and V in one loop, of batches of 4 or 8, 12.1.
 template <typename T, bool FOUR>
 __global__ __launch_bounds__(kStoreThreads) void k_prefix_load(DevState s, LoadArgs a, int group) {
   using V8 = typename Row8<T>::vec;
@@ -205,7 +204,7 @@ __global__ __launch_bounds__(kStoreThreads) void k_prefix_load(DevState s, LoadA
 }  // namespace
 
 hipError_t launch_store4(const DevState& s, const StoreArgs& a, hipStream_t st) {
-  const int group = store_group(a.n, a.n_layers);
+  const int group = store_group(a.n, a.n_layers, 2);
   const dim3 grid((a.n + group - 1) / group, a.n_layers);
 #define LAUNCH_STORE(T, AXES) hipLaunchKernelGGL((k_store4<T, AXES>), grid, dim3(kStoreThreads), 0, st, s, a, group)
   const bool f32 = s.dtype == TD_F32;
@@ -218,7 +217,7 @@ hipError_t launch_store4(const DevState& s, const StoreArgs& a, hipStream_t st) 
 }
 
 hipError_t launch_prefix_load(const DevState& s, const LoadArgs& a, hipStream_t st) {
-  const int group = store_group(a.n, a.n_layers);
+  const int group = store_group(a.n, a.n_layers, kStoreRows);
   const dim3 grid((a.n + group - 1) / group, a.n_layers);
 #define LAUNCH_LOAD(T, FOUR) hipLaunchKernelGGL((k_prefix_load<T, FOUR>), grid, dim3(kStoreThreads), 0, st, s, a, group)
   const bool f32 = s.dtype == TD_F32;

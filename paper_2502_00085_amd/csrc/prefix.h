@@ -96,7 +96,7 @@ struct LoadArgs {
   int four = 0;
 };
 hipError_t launch_prefix_load(const DevState& s, const LoadArgs& a, hipStream_t st);
-// Rows that one workgroup of a store or load takes.
-int store_group(long rows, int n_layers);
+// Rows that one workgroup of a store or load takes: `most` where there are enough, more only of very many.
+int store_group(long rows, int n_layers, int most);
 
 }  // namespace td

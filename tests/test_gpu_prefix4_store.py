@@ -72,6 +72,15 @@ def test_store(dtype, D, Hq, Hkv, r, inter, page, pos, n, axes):
     dec.close()
 
 
+@pytest.mark.parametrize("axes", [0, 3])
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,r,inter,page,pos,n", [
+    ("bf16", 64, 40, 40, 64, False, 64, 70, 2101), ("f32", 32, 96, 96, 32, True, 16, 3, 1025), ("bf16", 256, 40, 40, 256, False, 16, 9, 3),
+    ("f32", 128, 8, 8, 64, False, 128, 0, 4100)])
+def test_store_of_many(dtype, D, Hq, Hkv, r, inter, page, pos, n, axes):
+    """Several rows to a workgroup, the last one's fewer; more units of a row than a workgroup has threads for."""
+    test_store(dtype, D, Hq, Hkv, r, inter, page, pos, n, axes)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_borders(dtype):
     """Ties between sizes, largest values around the step of the unit, zeros of either sign, subnormal and huge
@@ -420,5 +429,46 @@ def test_refusals():
     with pytest.raises(ValueError):
         dec.prefix_store(0, 2, 0, k, k, rope=rope, positions=pos[:4])
     torch.cuda.synchronize()
+    assert dec.status() == 0
+    dec.close()
+
+
+@pytest.mark.parametrize("kind", ["4 bits", "plain"])
+def test_millions_of_tokens(kind):
+    """One call of more than four million tokens stores and loads what calls of parts of it do."""
+    n, page, D = 2 ** 22 + 3, 65536, 32
+    log(f"{kind} n={n}")
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    used = -(-n // page)
+    table = np.random.default_rng(7).permutation(used + 1)[:used]
+    shape = (used + 1, 1, 1, page)
+    if kind == "4 bits":
+        pages = [torch.zeros(shape + (w,), dtype=torch.uint8, device="cuda") for w in (D // 2, D // 32, D // 2, D // 32)]
+    else:
+        pages = [torch.zeros(shape + (D,), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    dec = B.TrieDecoder(1, 1, 4, 100, 1, 1, 1, D)
+    (dec.set_prefix4 if kind == "4 bits" else dec.set_prefix)(*pages, table, 0)
+    k, v, q = (torch.randn((1, n, 1, D), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(3))
+    rope = B.Rope(freqs(D))
+    out = torch.empty_like(q)
+    dec.prefix_store(0, 1, 0, k, v, q, out, rope)
+    stored = [p.clone() for p in pages]
+    back = [torch.empty_like(k) for _ in range(2)]
+    dec.prefix_load(0, 1, 0, *back)
+    for p in pages:
+        p.zero_()
+    part = torch.empty_like(q)
+    for a, e in ((0, 2 ** 21), (2 ** 21, n - 1), (n - 1, n)):
+        rows = [x[:, a:e].contiguous() for x in (k, v, q)]
+        turned = torch.empty_like(rows[2])
+        dec.prefix_store(0, 1, a, *rows, turned, rope)
+        part[:, a:e] = turned
+        some = [torch.empty_like(rows[0]) for _ in range(2)]
+        dec.prefix_load(0, 1, a, *some)
+        assert all(torch.equal(x, b[:, a:e]) for x, b in zip(some, back))
+    assert torch.equal(part, out)
+    assert all(torch.equal(p, s) for p, s in zip(pages, stored))
+    if kind == "plain":
+        assert torch.equal(back[1], v)
     assert dec.status() == 0
     dec.close()
