@@ -13,10 +13,11 @@
 //
 // What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape (201 MB in and out) in 40.7 us, 4.9 TB/s
 // (a copy's 4.9); with few rows one launch's latency (the leaves of 16 tries of 16 beams, 6.3 MB, 4.3 us; the
-// least 4.1).  Rows are read and written once; a WG has one, so that the angles are computed once
-// for its 32 to 48 heads.  With several rows to a WG the CUs end one after another (2 layers, eager, 1 / 2 / 4 / 8 rows, us:
-// 8,192 tokens 81.8 / 85.1 / 85.9 / 88.3; 16,000 149 / 156 / 160 / 172; 8 ragged prompts 64.3 / 64.1 / 71.5 / 76.7).  With several
-// axes the same: 6,001 tokens of a layer, 147 MB, 30.3 us, 4.9 TB/s.
+// least 4.1).  Rows are read and written once.  A WG has as many as give each of its threads a unit of two 16-byte
+// chunks, one of 32 to 48 heads: the angles are computed once for them, and with more rows the CUs end one after another.  2
+// layers of 20,000 tokens in bf16, 1 / 2 / 4 / 8 rows per WG, us: 28 q and 4 KV heads of 128 138 / 143 / 150 / 159; 8 and 8 of 128
+// 100 / 98 / 109 / 113; 16 and 4 of 64 53 / 43 / 42 / 43; 8 and 2 of 64 43 / 33 / 26 / 25; 8 ragged prompts of 32 and 8 of 128 64.3 /
+// 64.1 / 71.5 / 76.7.  With several axes the same: 6,001 tokens of a layer, 147 MB, 30.3 us, 4.9 TB/s.
 #include <algorithm>
 
 #include "kv_rows.h"
@@ -25,7 +26,7 @@ namespace td {
 
 namespace {
 
-// Grid (row groups, layers); a WG takes `group` consecutive rows (trie, j) of one layer: one, or of very many rows several.
+// Grid (row groups, layers); a WG takes `group` consecutive rows (trie, j) of one layer.
 template <typename T, bool AXES>
 __global__ __launch_bounds__(kStoreThreads) void k_store(DevState s, StoreArgs a, int group) {
   using C = StoreCfg<T>;
@@ -96,12 +97,13 @@ __global__ __launch_bounds__(kStoreThreads) void k_store(DevState s, StoreArgs a
 int store_group(long rows, int n_layers, int most) {
   // (as many rows per WG as leave a few WGs per CU, at most `most`; a grid of hundreds of millions of threads is long enough)
   if (rows > kStoreMany) return kStoreRows;
-  return (int)std::max(1l, std::min<long>(most, rows * n_layers / 1024));
+  return (int)std::max(1l, std::min<long>(std::min(most, kStoreRows), rows * n_layers / 1024));
 }
 
 hipError_t launch_store(const DevState& s, const StoreArgs& a, hipStream_t st) {
   const long rows = (long)a.tries * a.n;
-  const int group = store_group(rows, a.n_layers, 1);
+  const int units = ((a.q ? s.Hq : 0) + (a.k ? 2 * s.Hkv : 0)) * (s.D * (s.dtype == TD_F32 ? 4 : 2) / 32);
+  const int group = store_group(rows, a.n_layers, (kStoreThreads + units - 1) / units);
   const dim3 grid((rows + group - 1) / group, a.n_layers);
 #define LAUNCH_STORE(T, AXES) hipLaunchKernelGGL((k_store<T, AXES>), grid, dim3(kStoreThreads), 0, st, s, a, group)
   const bool f32 = s.dtype == TD_F32;

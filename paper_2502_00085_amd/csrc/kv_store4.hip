@@ -12,8 +12,11 @@
 // and no tie lies between it and the exact one.
 //
 // What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape, queries too (100 MB in, 76 out), 37.3 to 41 us, 4.3
-// to 4.7 TB/s (a copy's 4.9), with two rows to a WG; eight of them 40.8 to 44.5, one took 7 % longer (2 layers).  The 64-bit
-// sines are computed once for the 48 heads of a row; V's loads under way meanwhile changed nothing.
+// to 4.7 TB/s (a copy's 4.9), with two rows to a WG; eight of them 40.8 to 44.5.  A WG has as many rows as give each of its
+// threads at most 4 units (of 8 elements of K or V, or two 16-byte chunks of q).  2 layers stored and loaded in bf16, 1 / 2 / 4 / 8
+// rows, us: 8,192 tokens of 32 q and 8 KV heads of 128 104 / 101 / 106 / 106; 20,000 of 28 and 4 175 / 161 / - / 178; of 8 and 8
+// 166 / 147 / 138 / 143; of 8 and 2 of 64 - / 49 / 43 / 43.  The 64-bit sines are computed once for the heads of a row; V's loads
+// under way meanwhile changed nothing.
 #include <algorithm>
 
 #include "kv_rows.h"
@@ -204,7 +207,8 @@ __global__ __launch_bounds__(kStoreThreads) void k_prefix_load(DevState s, LoadA
 }  // namespace
 
 hipError_t launch_store4(const DevState& s, const StoreArgs& a, hipStream_t st) {
-  const int group = store_group(a.n, a.n_layers, 2);
+  const int units = (a.k ? 2 * s.Hkv * (s.D / 8) : 0) + (a.q ? s.Hq * (s.D * (s.dtype == TD_F32 ? 4 : 2) / 32) : 0);
+  const int group = store_group(a.n, a.n_layers, 4 * kStoreThreads / units);
   const dim3 grid((a.n + group - 1) / group, a.n_layers);
 #define LAUNCH_STORE(T, AXES) hipLaunchKernelGGL((k_store4<T, AXES>), grid, dim3(kStoreThreads), 0, st, s, a, group)
   const bool f32 = s.dtype == TD_F32;
