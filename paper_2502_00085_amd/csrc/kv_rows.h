@@ -31,7 +31,7 @@ __device__ inline StoreRow store_row(const DevState& s, const StoreArgs& a, cons
     // other kind)
     if (a.pos0 + j < p.room) {
       w.position = a.pos0 + j;
-      const int64_t page = p.table[w.position >> p.shift];
+      const int64_t page = ((const TD_GLOBAL int32_t*)(uintptr_t)p.table)[w.position >> p.shift];
       w.dst = (((page * s.L + lab) * s.Hkv) << p.shift) + (w.position & ((1 << p.shift) - 1));
     } else {
       set_status(s.status, kDevEinval);
@@ -61,7 +61,8 @@ __device__ inline double pair_position(const StoreArgs& a, int r, int own, int p
 }
 
 // Unit w of a head: E pairs of its first `rotary` elements, or 2 E copied ones, from src to out, which may
-// be the same.  turn(pair): cosine and sine.
+// be the same.  turn(pair): cosine and sine.  (Global accesses: a flat store, of an address chosen among pools,
+// pages and q_out, also counts as one to LDS.)
 template <typename T, typename Turn>
 __device__ inline void store_unit(const T* src, T* out, int w, int turned, bool rotate, bool interleaved, Turn&& turn) {
   using C = StoreCfg<T>;
@@ -69,7 +70,9 @@ __device__ inline void store_unit(const T* src, T* out, int w, int turned, bool 
   constexpr int E = C::E;
   const bool split = rotate && !interleaved;
   const int c0 = split ? w : 2 * w, c1 = split ? w + turned : 2 * w + 1;
-  const V x = reinterpret_cast<const V*>(src)[c0], y = reinterpret_cast<const V*>(src)[c1];
+  const TD_GLOBAL V* const from = (const TD_GLOBAL V*)(uintptr_t)src;
+  TD_GLOBAL V* const to = (TD_GLOBAL V*)(uintptr_t)out;
+  const V x = from[c0], y = from[c1];
   V x1 = x, y1 = y;
   if (rotate) {
     if (split) {
@@ -92,8 +95,8 @@ __device__ inline void store_unit(const T* src, T* out, int w, int turned, bool 
       }
     }
   }
-  reinterpret_cast<V*>(out)[c0] = x1;
-  reinterpret_cast<V*>(out)[c1] = y1;
+  to[c0] = x1;
+  to[c1] = y1;
 }
 
 }  // namespace td
