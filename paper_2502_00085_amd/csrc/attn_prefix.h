@@ -42,7 +42,8 @@ __device__ inline PrefixUnit prefix_unit(const DevState& s, const PrefixArgs& a)
   return u;
 }
 
-// A call captured with a prefix of one kind finds nothing to read where one of the other is attached.
+// A call captured with a prefix of one kind finds nothing to read where one of the other is attached.  (Called
+// behind the first loads: it waits for the header.)
 __device__ inline void prefix_other_kind(const DevState& s, const PrefixHdr& p) {
   if (p.other != 0 && blockIdx.x == 0 && threadIdx.x == 0) set_status(s.status, kDevEinval);
 }

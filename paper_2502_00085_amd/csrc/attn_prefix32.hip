@@ -53,7 +53,6 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
   __shared__ int wred[4 * RW];
   __shared__ float ml[KW == 2 ? RW * 128 : 1];
   const PrefixHdr p = s.prefix[FOUR ? 1 : 0];
-  prefix_other_kind(s, p);
   const PrefixUnit u = prefix_unit(s, a);
   const int lab = a.layer_begin + u.li;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -171,6 +170,7 @@ __global__ __launch_bounds__(64 * RW * KW, (Prefix32Cfg<D, RW, KW>::WAVES)) void
     else issue(0, pages_of(0));
     if (n_tiles > 1) next = pages_of(1);
   }
+  prefix_other_kind(s, p);
   if (known) {
     prefix_row_keys(s, a, p, q);
     span = prefix_span(q);

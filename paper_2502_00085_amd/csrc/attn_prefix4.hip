@@ -154,7 +154,6 @@ template <typename T, int D>
 __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, const PrefixArgs& a, unsigned char* vbuf, float* ml) {
   using C = FewCfg<D>;
   const PrefixHdr p = s.prefix[1];
-  prefix_other_kind(s, p);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hh = lane >> 5;
@@ -221,6 +220,7 @@ __device__ __attribute__((always_inline)) inline void few_wg(const DevState& s, 
     fetch(tile_of(1), pg1, k1, v1);
     next = pages_of(tile_of(2));
   }
+  prefix_other_kind(s, p);
   if (known) {
     prefix_row_keys(s, a, p, q);
     span = prefix_span(q);

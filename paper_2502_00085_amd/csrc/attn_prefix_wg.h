@@ -63,7 +63,6 @@ __device__ __attribute__((always_inline)) inline void prefix_wg(
   constexpr bool TRIES = WGS != Wgs::kPrefix;
   using T4 = Tile4<D, C::THREADS, 64>;
   PrefixHdr p = s.prefix[FOUR ? 1 : 0];
-  prefix_other_kind(s, p);
   const bool trie = WGS == Wgs::kTries || (WGS == Wgs::kBoth && blockIdx.x >= a.prefix_wgs);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -249,6 +248,7 @@ __device__ __attribute__((always_inline)) inline void prefix_wg(
     }
     if (m0 + 2 < m1) next = pages_of(m0 + 2);
   }
+  prefix_other_kind(s, p);
   if (TRIES && trie) {
     if (q.in && q.j < th.n_live) {
       q.lo = all.lo;
