@@ -159,47 +159,8 @@ __global__ __launch_bounds__(kMergeThreads) void k_prefix_merge(DevState s, Pref
 
 }  // namespace
 
-// A 4-bit pass takes its rows 32 at a time (k_attn_prefix4_few) in bf16 up to 512 of them and d = 128.  Measured
-// against blocks of up to 128, us, with the splits below, 8 KV heads at d = 128 unless stated: 64 rows over 4,096
-// keys 17.1 and 18.7, over 30,000 29.6 and 35; 128 rows 19.7 and 22.5, 40.3 and 42.6; 512 rows 30.7 and 33.1, over
-// 20,000 77.9 and 75.3; 1,024 rows 43.4 and 43.2, 125 and 119; 32 KV heads, 128 rows over 20,000 73.4 and 87; at d = 256
-// 256 rows over 20,000 99 and 69.  In fp32 any number up to d = 192, against the fp32 matrix instructions
-// (k_attn_prefix32): d = 128, 128 rows over 8,000 45.6 and 104; d = 192, 4 KV heads, 57 and 84; d = 256, 116 and 102.
-static bool few_rows(const DevState& s, bool four, long rows) {
-  return four && (s.dtype == TD_F32 ? s.D <= 192 : s.D <= 128 && rows <= 512);
-}
-int prefix_rows_per_block(const DevState& s, bool four, long rows) {
-  if (few_rows(s, four, rows)) return 32;
-  return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-}
-
-// A WG per CU, of at least 4 tiles of 64 keys; two per CU where each still has 16.  More splits make
-// shorter chains of tiles and more records to merge.  Measured, 8 KV heads at d = 128, the pass and
-// its merge, us: 128 rows over 4,096 keys, 8 / 16 / 32 splits: 22.6 / 20.9 / 24.6; over 16,384 keys, 16 /
-// 32 / 64: 35.1 / 30.5 / 34.1; 1,024 rows (8 blocks) over 1,024 keys, 4 / 8: 25.5 / 27.7; over 8,192 keys,
-// 4 / 8 / 16: 63 / 57 / 72; 32 rows over 4,096 keys, 16 / 32 / 64: 17.4 / 17.9 / 20.1.  In fp32 a tile takes
-// ten times as long: one tile, and two per CU where each still has 2.
-//
-// In 4 bits (blocks of 32 rows, d <= 128) a record costs as much as before and a tile a quarter of the memory's
-// time: of at least 6 tiles where 16 units or more write records, and two per CU where each still has 64.  us:
-// 32 rows over 4,096 keys, 4 / 8 / 16 / 32 splits: 21.3 / 16.4 / 16.6 / 21.3; 64 rows, 4 / 8 / 12 / 16: 19.3 /
-// 17.1 / 17.5 / 21.2; 128 rows, 4 / 6 / 8 / 12: 19.7 / 19.9 / 21.5 / 22.6, over 30,000, 4 / 8 / 16: 59 / 40.3 / 45.3; 32
-// KV heads, 8 rows over 30,000, 4 / 8 / 16: 60.5 / 39.3 / 42.8; 128 rows over 20,000 (313 tiles), 2 / 4: 85 / 73.4.
-int prefix_splits(const DevState& s, bool four, long units, long keys, long most) {
-  const long tiles = (keys + 63) / 64;
-  if (few_rows(s, four, 0)) {
-    const long least = units < 16 ? 4 : 6;
-    const long one = std::min(256 / units, (tiles + least - 1) / least);
-    const long two = s.dtype == TD_F32 && s.D >= 128 ? 0 : std::min(512 / units, tiles / 64);  // (fp32: one fits a CU)
-    return (int)std::max(1l, std::min(std::max(one, two), most));
-  }
-  const long few = s.dtype == TD_F32 ? 1 : 4, many = s.dtype == TD_F32 ? 2 : 16;
-  const long one = std::min((256 + units - 1) / units, tiles / few), two = std::min((512 + units - 1) / units, tiles / many);
-  return (int)std::max(1l, std::min(std::max(one, two), most));
-}
-
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
-  const int rpb = prefix_rows_per_block(s, a.four, (long)a.tries * a.per_trie * (s.Hq / s.Hkv));
+  const int rpb = prefix_rows_per_block(prefix_heads(s), a.four, (long)a.tries * a.per_trie * (s.Hq / s.Hkv));
   if (a.trie_splits > 0 && (a.rows != PrefixRows::kLeaves || s.dtype != TD_BF16 || !mfma_head_dim(s.D))) return hipErrorInvalidValue;
   if (a.four) return launch_prefix4(s, a, rpb, st, ev0, ev1);
   if (s.dtype == TD_F32) return launch_prefix32(s, a, rpb, st, ev0, ev1);

@@ -18,9 +18,6 @@ namespace {
 // Records an attention launch merges by itself, one after the other: more are merged by a launch of
 // their own, eight at a time.
 constexpr int kFoldSplits = 4;
-constexpr long kOneRound = 512;  // WGs of a pass that run at once (two per CU)
-constexpr long kTrieTiles = 8;
-constexpr long kShortPass = 16;  // tiles of the prefix per WG
 constexpr long kSmallBlocks = 1 << 20;  // blocks of 32 rows (of a layer) per launch
 constexpr int kStoreRows = 1 << 26;  // rows per layer of a store (what a launch's grid holds)
 constexpr size_t kWorkFloats = 16u << 20;  // of either workspace, unless one layer needs more
@@ -112,59 +109,18 @@ hipError_t prefix_pass(td_ctx* c, bool nodes, int layer_begin, int n_layers, int
   a.q0 = q0;
   a.q_stride = q_max;
   a.scale_log2 = scale_log2;
-  const long rows = (long)s.T * qn * (s.Hq / s.Hkv);
-  const int rpb = prefix_rows_per_block(s, c->prefix_four, rows);
-  a.row_blocks = (int)((rows + rpb - 1) / rpb);
+  a.four = c->prefix_four;
   const long keys = s.W > 0 ? std::min(c->prefix_length, s.W) : c->prefix_length;
   const long fit = (long)(c->prefix_records / ((size_t)n_layers * s.T * qn * s.Hq));
-  a.four = c->prefix_four;
-  a.splits = prefix_splits(s, a.four && rpb == 32, (long)n_layers * s.Hkv * a.row_blocks, keys, std::min<long>(fit, max_splits));
-  // In 4 bits, row blocks that read the same keys belong on one XCD, if that costs less than a fifth of the splits (us, over
-  // 30,000 positions: 16 beams, 4 KV heads, d = 64, 30 splits 20.1, 31 21.5; 8 x 16 beams, 28 heads and 4 KV heads, d = 128,
-  // 97.5 and 124.6; 8 x 16 beams of 6 heads, d = 96, 8 splits 38.7, 10 36.3).
-  auto group = [&]() {
-    for (int i = a.splits; a.four && a.row_blocks > 1 && 5 * i > 4 * a.splits; --i)
-      if ((long)n_layers * s.Hkv * i % 8 == 0) {
-        a.splits = i;
-        break;
-      }
-  };
-  group();
-  *tries = false;
-  if (trie_nodes > 0) {
-    // the tries' own nodes in the same launch, where all of its WGs run at once, none has more than
-    // kTrieTiles tiles of a trie, and the pass itself is short.  Measured over 210 shapes (1 to 16 tries of 2 to
-    // 32 beams and 40 to 5,000 nodes, 64 to 50,000 positions, d = 64 to 128; graphs of one-layer calls): within
-    // these limits 21 % less time than with launches of their own (4 x 8 beams of 266 nodes over 4,096
-    // positions 22.1 us a layer against 30.3), at worst 4 % more (2 x 32 of 229 over 64: 21.9, 21.1).  Past
-    // kTrieTiles, 11 % less to 12 % more.  The other two limits keep away from what was not measured, calls of
-    // many layers, and cost one-layer calls past them 7 % (2 x 4 beams of 404 nodes over 50,000 positions, 32 KV
-    // heads, 49 tiles of the prefix per WG: 117.8, 127.2).  In 4 bits the pass may be long: 8 rows of 32 KV heads
-    // over 30,000 positions 38.9 us in one launch of 8 or 12 splits, 42.7 in two of 16.
-    // A trie's WG has 3 of its tiles, which take about as long as the 4 that a WG of the prefix has at least:
-    // over 160 of these shapes 1 or 2 took 1.4 % less in the mean, 4 took 4 % more, 6 8 %, 8 13 %.
-    const long unit = (long)n_layers * s.Hkv * a.row_blocks, tiles = (trie_nodes + 63) / 64, prefix_tiles = (keys + 63) / 64;
-    const int tr = a.four && rpb == 32 ? kFewTrieRows : rpb;  // a trie's rows of a WG
-    const long blocks = (qn * (s.Hq / s.Hkv) + tr - 1) / tr, units = (long)n_layers * s.T * s.Hkv * blocks;
-    const long ts = std::max(1l, std::min({(tiles + 2) / 3, 256 / units, fit - a.splits}));
-    // In 4 bits and blocks of 32 rows a short pass leaves CUs to the tries (128 rows over 4,096 keys, 6 splits 19.9 us, 8
-    // 21.5; 64 rows over 8,000, 14 22.8, 16 25.1; 8 rows of 32 KV heads, d = 96, over 8,000, 21 tiles per WG, 6 23.8, 8
-    // 22.5).
-    const long left = std::max(0l, 256 - units * ts) / unit;
-    if (a.four && rpb == 32 && prefix_tiles <= kShortPass * left && left < a.splits) {
-      a.splits = (int)left;
-      group();
-    }
-    const long wgs = unit * a.splits;
-    if (wgs + units * ts <= kOneRound && (a.four || prefix_tiles <= kShortPass * a.splits) && (tiles + ts - 1) / ts <= kTrieTiles && a.splits + ts <= fit) {
-      a.trie_splits = (int)ts;
-      a.trie_blocks = (int)blocks;
-      a.prefix_wgs = (uint32_t)wgs;
-      *tries = true;
-    }
-  }
+  const PassShape shape = prefix_pass_shape(prefix_heads(s), a.four, n_layers, qn, keys, fit, max_splits, trie_nodes);
+  a.row_blocks = shape.row_blocks;
+  a.splits = shape.splits;
+  a.xcd_group = shape.xcd_group;
+  a.trie_splits = shape.trie_splits;
+  a.trie_blocks = shape.trie_blocks;
+  a.prefix_wgs = (uint32_t)shape.prefix_wgs;
   a.records = a.splits + a.trie_splits;
-  a.xcd_group = a.row_blocks > 1 && ((long)n_layers * s.Hkv * a.splits) % 8 == 0;
+  *tries = shape.trie_splits > 0;
   *splits = a.records;
   return launch_prefix(s, a, st, ev0, nullptr);
 }
@@ -403,7 +359,8 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
   if ((int64_t)n * G > (1 << 24)) return fail(c, TD_EINVAL, "n must be at most 2^24 / (Hq / Hkv)");
   if (td_status r = other_device(c)) return r;
   const long rows = (long)n * G;
-  const int rpb = td::prefix_rows_per_block(s, c->prefix_four, rows), blocks = (int)((rows + rpb - 1) / rpb);
+  const td::PrefixHeads heads = td::prefix_heads(s);
+  const int rpb = td::prefix_rows_per_block(heads, c->prefix_four, rows), blocks = (int)((rows + rpb - 1) / rpb);
   // (as many layers per launch as its grid holds)
   const int lc = (int)std::max(1l, std::min<long>(n_layers, (1l << 22) / ((long)s.Hkv * blocks)));
   // (and as many queries: blocks of 32 rows, which a 4-bit pass in fp32 takes any number of, may come to more)
@@ -430,13 +387,13 @@ td_status trie_prefix_attn(td_ctx* c, int32_t layer_begin, int32_t n_layers, int
       a.row_blocks = qc == n ? blocks : (int)(((long)a.per_trie * G + rpb - 1) / rpb);
       const long keys = s.W > 0 ? std::min(pos + n, s.W) : pos + n, units = (long)a.n_layers * s.Hkv * a.row_blocks;
       const long fit = qc == n ? (long)(c->prefix_records / ((size_t)a.n_layers * n * s.Hq)) : 1;
-      a.records = a.splits = td::prefix_splits(s, a.four && rpb == 32, units, keys, std::max(1l, fit));
-      a.xcd_group = a.row_blocks > 1 && ((long)a.n_layers * s.Hkv * a.splits) % 8 == 0;
+      a.records = a.splits = td::prefix_splits(heads, a.four && rpb == 32, units, keys, std::max(1l, fit));
+      a.xcd_group = a.row_blocks > 1 && td::prefix_xcd_eights(a.n_layers, s.Hkv, a.splits);
       // Two WGs per CU at once, and no third: a long block beside a short one.  2,048 tokens of 32 heads (8
       // KV heads, d = 128) from position 0: 57.5 -> 53.7 us a layer, from 6,144: 254 -> 247.5 (graphs in turn);
       // where fewer CUs have two (1,500 tokens) 42.4 -> 41.4 from 0, 210.4 and 210.7 from 6,144.  With more WGs the
       // longest first fill the CUs evenly by themselves.
-      a.pair_blocks = s.D <= 128 && units * a.splits > kOneRound / 2 && units * a.splits <= kOneRound;
+      a.pair_blocks = s.D <= 128 && units * a.splits > td::kOneRound / 2 && units * a.splits <= td::kOneRound;
       a.part_o = a.splits > 1 ? c->prefix_o : nullptr;
       a.part_ml = c->prefix_ml;
       hipEvent_t last = l + lc >= n_layers && q0 + qc >= n ? ev1 : nullptr;

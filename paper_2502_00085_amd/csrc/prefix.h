@@ -1,6 +1,7 @@
 // The shared prefix: arguments of its attention pass and of the K/V stores, and the launchers.
 #pragma once
 
+#include "prefix_rule.h"
 #include "td_internal.h"
 
 namespace td {
@@ -42,16 +43,11 @@ struct PrefixArgs {
   uint32_t prefix_wgs = 0;
 };
 
-// Query rows of a workgroup for a pass of this many rows per KV head (four: over 4-bit pages).
-int prefix_rows_per_block(const DevState& s, bool four, long rows);
-// Splits of `keys` keys for `units` (layer, KV head, row block) units, at most `most` (four: over 4-bit pages, in blocks
-// of 32 rows).
-int prefix_splits(const DevState& s, bool four, long units, long keys, long most);
+inline PrefixHeads prefix_heads(const DevState& s) { return {s.T, s.Hq, s.Hkv, s.D, s.dtype == TD_F32}; }
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_prefix32(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
                            hipEvent_t ev1);
 
-constexpr int kFewTrieRows = 64;  // rows of a trie's WG beside a 4-bit pass in blocks of 32 rows
 hipError_t launch_prefix4(const DevState& s, const PrefixArgs& a, int rows_per_block, hipStream_t st, hipEvent_t ev0,
                           hipEvent_t ev1);
 
