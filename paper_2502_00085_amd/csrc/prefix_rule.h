@@ -15,6 +15,7 @@ struct PrefixHeads {
 
 constexpr long kOneRound = 512;   // WGs of a pass that run at once (two per CU)
 constexpr long kTrieTiles = 8;
+constexpr long kMostTrieTiles = 6;  // of a trie's WG beside a short 4-bit pass
 constexpr long kShortPass = 16;   // tiles of the prefix per WG
 constexpr int kFewTrieRows = 64;  // rows of a trie's WG beside a 4-bit pass in blocks of 32 rows
 
@@ -107,15 +108,25 @@ inline PassShape prefix_pass_shape(const PrefixHeads& s, bool four, int n_layers
     const long tiles = (trie_nodes + 63) / 64, prefix_tiles = (keys + 63) / 64;
     const int tr = few ? kFewTrieRows : rpb;  // a trie's rows of a WG
     const long blocks = ((long)per_trie * G + tr - 1) / tr, units = (long)n_layers * s.tries * s.kv_heads * blocks;
-    const long ts = std::max(1l, std::min({(tiles + 2) / 3, 256 / units, fit - a.splits}));
+    long ts = std::max(1l, std::min({(tiles + 2) / 3, 256 / units, fit - a.splits}));
     // In 4 bits and blocks of 32 rows a short pass leaves CUs to the tries (128 rows over 4,096 keys, 6 splits 19.9 us, 8
     // 21.5; 64 rows over 8,000, 14 22.8, 16 25.1; 8 rows of 32 KV heads, d = 96, over 8,000, 21 tiles per WG, 6 23.8, 8
-    // 22.5).  A longer one keeps its splits: as many as make its WGs short again took 0.2 % more in the mean over 147
-    // captured one-layer calls on both sides of the limit (1 to 8 tries of 4 to 16 beams over 1,000 to 16,000 positions;
-    // 8 % less to 8 % more).
+    // 22.5).  Where that would leave it too few to be short, a trie's WGs have up to 6 tiles instead (4 x 8 beams over
+    // 4,096 keys, 4 layers, 14 tiles of a trie: 8 splits beside 5 88.9 us, 4 beside 4 83.5, 4 beside 5 88.6; 64 rows
+    // of 8 KV heads over 2,500 23.0 and 20.0; 287 captured one-layer calls of 1 to 8 tries over 1,000 to 16,000 keys: 15 %
+    // less to 3 % more; with up to 9 tiles up to 42 % more, with up to 4 a quarter of the gain), and past that it keeps
+    // its splits.
     int splits = a.splits;  // (of a pass that the tries join; alone it keeps its own)
-    const long left = std::max(0l, 256 - units * ts) / unit;
-    if (few && prefix_tiles <= kShortPass * left && left < splits) splits = grouped((int)left);
+    const long least = (prefix_tiles + kShortPass - 1) / kShortPass;  // splits of a short pass
+    long left = std::max(0l, 256 - units * ts) / unit;
+    if (few && left < least && least < splits) {
+      const long fewer = (256 - unit * least) / units;
+      if (fewer >= 1 && tiles <= kMostTrieTiles * fewer) {
+        ts = fewer;
+        left = (256 - units * ts) / unit;
+      }
+    }
+    if (few && least <= left && left < splits) splits = grouped((int)left);
     const long wgs = unit * splits;
     if (wgs + units * ts <= kOneRound && (four || prefix_tiles <= kShortPass * splits) && (tiles + ts - 1) / ts <= kTrieTiles &&
         splits + ts <= fit) {

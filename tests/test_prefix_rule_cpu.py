@@ -82,3 +82,25 @@ def test_limits_of_a_launch(shape):
             rows = 64 if four else (32 if tries * beams * G <= 32 else 64 if tries * beams * G <= 64 else 128)
             if not four or tries * beams * G <= 512:
                 assert a.trie_blocks * rows >= beams * G, case
+
+
+def test_a_short_pass_stays_short_as_the_tries_grow(shape):
+    """A captured call goes by the tries' capacity, the same call outside a graph by the nodes that they have: a few more
+    nodes change a short pass's splits by little, and it stays within a workgroup per CU."""
+    # 4 x 8 beams of 32 heads (8 KV heads) over 4,096 positions, 736 nodes stored, room for 868
+    for nodes in (736, 868):
+        a = shape(4, 8, 4, 8, 128, 4096, nodes)
+        assert (a.splits, a.trie_splits) == (4, 4), nodes
+    for tries, beams, G, kv, keys in ((4, 8, 4, 8, 4096), (4, 16, 4, 8, 2500), (8, 8, 4, 8, 1000), (4, 8, 4, 8, 6000), (2, 4, 1, 32, 1000)):
+        before, tiles = None, 0
+        while True:
+            tiles += 1
+            a = shape(tries, beams, G, kv, 128, keys, 64 * tiles)
+            wgs = a.prefix_wgs + tries * kv * a.trie_blocks * a.trie_splits
+            if a.trie_splits == 0 or wgs > 256:
+                break  # (the tries are too large for it)
+            case = (tries, beams, G, kv, keys, tiles, a)
+            assert a.splits >= min(shape(tries, beams, G, kv, 128, keys, 0).splits, -(-keys // 64 // 16)), case
+            assert before is None or abs(a.splits - before) <= 2, case
+            before = a.splits
+        assert tiles > 12, (tries, beams, keys, tiles)
