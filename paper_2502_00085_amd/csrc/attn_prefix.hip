@@ -159,7 +159,16 @@ __global__ __launch_bounds__(kMergeThreads) void k_prefix_merge(DevState s, Pref
 
 }  // namespace
 
+// What the kernels take for granted of a launch: a WG takes its number apart (prefix_unit) into a layer, a KV head, a
+// row block and a split, which address the pages, the pools and the records.
+static bool launch_fits(const DevState& s, const PrefixArgs& a) {
+  return a.splits >= 1 && a.row_blocks >= 1 && a.n_layers >= 1 && a.layer_begin >= 0 && a.layer_begin + a.n_layers <= s.L &&
+         a.records >= a.splits + a.trie_splits && (!a.xcd_group || prefix_xcd_eights(a.n_layers, s.Hkv, a.splits)) &&
+         (a.trie_splits == 0 || a.prefix_wgs == (uint64_t)a.n_layers * s.Hkv * a.row_blocks * a.splits);
+}
+
 hipError_t launch_prefix(const DevState& s, const PrefixArgs& a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
+  if (!launch_fits(s, a)) return hipErrorInvalidValue;
   const int rpb = prefix_rows_per_block(prefix_heads(s), a.four, (long)a.tries * a.per_trie * (s.Hq / s.Hkv));
   if (a.trie_splits > 0 && (a.rows != PrefixRows::kLeaves || s.dtype != TD_BF16 || !mfma_head_dim(s.D))) return hipErrorInvalidValue;
   if (a.four) return launch_prefix4(s, a, rpb, st, ev0, ev1);
