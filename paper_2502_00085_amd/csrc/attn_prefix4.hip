@@ -9,12 +9,12 @@
 //     in bf16: 2,048 tokens from position 6,144 (8 KV heads, 32 query heads, d = 128) 237 us a layer, 1,012 TFLOP/s
 //     (without a trace 232, 1,036; the bf16 prefix 241, a library product 1,252).
 //   * Fewer (a decode step): k_attn_prefix4_few, in blocks of 32 rows.  HBM where the prefix is long: 8 rows of 32
-//     KV heads, d = 96, over 50,001 positions 36.4 us, 4.5 TB/s (a copy's 4.9), 43 with the tries' nodes in the launch
+//     KV heads, d = 96, over 50,001 positions 36.4 us, 4.5 TB/s (a copy's 4.9), 43.5 with the tries' nodes in the launch
 //     (the bf16 pass 108 to 112).  Below some 4,000 keys per KV head a chain of latencies, as in bf16: 128 rows of 8 KV
-//     heads over 4,096 keys, with the tries' nodes, 16.9 us (its 4.5 MB take 0.9, its records 2 to 3).
+//     heads over 4,096 keys, with the tries' nodes, 16.1 us (its 4.5 MB take 0.9, its records 2 to 3).
 //   * fp32: the same kernel, the queries and the weights as three bf16 parts each (24 bits: all of them), three products
 //     for one.  These run at 5 times the rate of the fp32 matrix instructions or more: 700 tokens from position
-//     3,000 (32 heads, d = 128) 134 us against 520; 128 rows of 8 KV heads over 8,000 keys 23.6 against 80.
+//     3,000 (32 heads, d = 128) 130 us against 520; 128 rows of 8 KV heads over 8,000 keys 23.6 against 80.
 // Tried and not kept: eight waves per WG (the same to 1 %; more than 256 registers a wave past d = 128); one tile's loads
 // under way instead of two, which the compiler made of them while the queries' loads were not waited for ahead of the
 // loop (48.9 us for the 36.4 above).
@@ -39,8 +39,9 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   else prefix_wg<D, RW, KW, Wgs::kPrefix, true>(s, a, kbuf0, vbuf0, kbuf1, vbuf1, wred, ml);
 }
 
-// Up to 32 rows per KV head: no other wave needs a wave's keys.  Each of the four waves of a WG streams tiles of
-// 32 keys of its own, without a barrier until the end: K goes from memory to the first product's operand
+// Blocks of 32 rows: no other wave of the WG needs a wave's keys.  (The row blocks of a KV head read and convert the same
+// keys each for itself, from one XCD's L2 where they lie there: PrefixArgs::xcd_group.)  Each of the four waves of a
+// WG streams tiles of 32 keys of its own, without a barrier until the end: K goes from memory to the first product's operand
 // through registers alone (lane: half a row, as S^T = K Q^T takes it), V through 32 rows of LDS that the wave has
 // for itself (written row by row, read transposed).  Two tiles are under way per wave.
 constexpr int kFewWaves = 4;

@@ -11,13 +11,13 @@
 // The angle of a far position needs more than fp32: p f_i in turns, in 64 bits, less whole turns;
 // the sine and cosine of the rest in fp32, once per (row, pair), in LDS for all of the row's heads.
 //
-// What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape (201 MB in and out) in 40.7 us, 4.9 TB/s
-// (a copy's 4.9); with few rows one launch's latency (the leaves of 16 tries of 16 beams, 6.3 MB, 4.3 us; the
-// least 4.1).  Rows are read and written once.  A WG has as many as give each of its threads a unit of two 16-byte
+// What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape (201 MB in and out) in 40.0 us, 5.0 TB/s
+// (a copy's 4.9); with few rows one launch's latency (the leaves of 16 tries of 16 beams, 6.3 MB, 4.3 us, the
+// least 4.1; with several axes 5.0 and 4.7).  Rows are read and written once.  A WG has as many as give each of its threads a unit of two 16-byte
 // chunks, one of 32 to 48 heads: the angles are computed once for them, and with more rows the CUs end one after another.  2
 // layers of 20,000 tokens in bf16, 1 / 2 / 4 / 8 rows per WG, us: 28 q and 4 KV heads of 128 138 / 143 / 150 / 159; 8 and 8 of 128
 // 100 / 98 / 109 / 113; 16 and 4 of 64 53 / 43 / 42 / 43; 8 and 2 of 64 43 / 33 / 26 / 25; 8 ragged prompts of 32 and 8 of 128 64.3 /
-// 64.1 / 71.5 / 76.7.  With several axes the same: 6,001 tokens of a layer, 147 MB, 30.3 us, 4.9 TB/s.
+// 64.1 / 71.5 / 76.7.  With several axes the same: 6,001 tokens of a layer, 147 MB, 30.6 us, 4.8 TB/s.
 #include <algorithm>
 
 #include "kv_rows.h"
