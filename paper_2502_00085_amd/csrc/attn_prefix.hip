@@ -35,7 +35,8 @@ namespace td {
 
 namespace {
 
-template <int D, int RW, int KW, bool TRIES>
+// NODES: the launch's last WGs take the tries' own nodes.
+template <int D, int RW, int KW, bool NODES>
 __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k_attn_prefix(DevState s, PrefixArgs a) {
   // (an array per buffer: the compiler can tell an operand read of one buffer from the direct loads
   // under way into the others)
@@ -44,7 +45,13 @@ __global__ __launch_bounds__(64 * RW * KW, (PrefixCfg<D, RW, KW>::WAVES)) void k
   __shared__ __attribute__((aligned(16))) unsigned char kbuf1[BUF], vbuf1[BUF];
   __shared__ int wred[4 * RW];
   __shared__ float ml[KW == 2 ? RW * 128 : 1];
-  prefix_wg<D, RW, KW, TRIES ? Wgs::kBoth : Wgs::kPrefix, false>(s, a, kbuf0, vbuf0, kbuf1, vbuf1, wred, ml);
+  if constexpr (NODES) {
+    prefix_wg<D, RW, KW, Wgs::kBoth, false>(s, a, kbuf0, vbuf0, kbuf1, vbuf1, wred, ml);
+  } else {
+    constexpr Wgs WGS = Wgs::kPrefix;
+    constexpr bool FOUR = false;
+#include "attn_prefix_body.h"
+  }
 }
 
 template <int D>

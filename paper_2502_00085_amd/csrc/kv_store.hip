@@ -13,8 +13,8 @@
 //
 // What bounds it: HBM.  8,192 tokens of a layer at the Llama-8B shape (201 MB in and out) in 40.0 us, 5.0 TB/s
 // (a copy's 4.9); with few rows one launch's latency (the leaves of 16 tries of 16 beams, 6.3 MB, 4.3 us, the
-// least 4.1; with several axes 5.0 and 4.7).  Rows are read and written once.  A WG has as many as give each of its threads a unit of two 16-byte
-// chunks, one of 32 to 48 heads: the angles are computed once for them, and with more rows the CUs end one after another.  2
+// least 4.1; with several axes 5.0 and 4.7).  Rows are read and written once.  A WG has as many as give each of its
+// threads a unit of two 16-byte chunks, one of 32 to 48 heads: the angles are computed once for them, and with more rows the CUs end one after another.  2
 // layers of 20,000 tokens in bf16, 1 / 2 / 4 / 8 rows per WG, us: 28 q and 4 KV heads of 128 138 / 143 / 150 / 159; 8 and 8 of 128
 // 100 / 98 / 109 / 113; 16 and 4 of 64 53 / 43 / 42 / 43; 8 and 2 of 64 43 / 33 / 26 / 25; 8 ragged prompts of 32 and 8 of 128 64.3 /
 // 64.1 / 71.5 / 76.7.  With several axes the same: 6,001 tokens of a layer, 147 MB, 30.6 us, 4.8 TB/s.
